@@ -1,0 +1,75 @@
+/*
+ * metok_decode.h -- C ABI of the decoding-time operators beside stage 3 (AMD MI355X, gfx950).
+ *
+ * Stage 3 of METok (arXiv 2506.02850, Sec. 3.3) leaves a compacted KV cache (Eq. 3); while the answer is written, every new token
+ * attends to it and adds a row:
+ *   - the attention of one new token per video over a dense or paged cache, which appends the token's own row and, if asked,
+ *     adds up how much attention every cached row draws (the decoding-time counterpart of the stage-2 score, Sec. 3.2.2).
+ * The conventions of metok.h hold (caller-owned buffers, no synchronisation, deterministic results, capture into HIP graphs after
+ * one ordinary call, error codes, 16-byte alignment, finite inputs).  Two additions:
+ *   - Lengths live on the device, so that a captured decoding step can be replayed while the caches grow.  A length below 0 counts
+ *     as 0 and one above the capacity as the capacity.
+ *   - A workspace may be shared by calls that follow each other (on one stream, or in graphs that are replayed one after the
+ *     other); calls that may overlap in time need workspaces of their own.
+ */
+#ifndef METOK_DECODE_H
+#define METOK_DECODE_H
+
+#include "metok.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+#define METOK_MAX_DECODE_BATCH 4096   /* B limit of the calls below */
+
+/* ---------------------------------------------------------------------------------------------
+ * Attention of one new token per video over the KV cache.
+ *
+ *   q            device, [B, Hq, dh] of `dtype`: the new token's queries.  Query head h reads kv head h / (Hq / Hkv).
+ *   k_cache, v_cache  device, one layer's cache [B, Hkv, S_cap, dh] of `dtype` (the layout of metok_kv_compact).
+ *   len          device, [B] int32: rows every video's cache holds before this call.  Not modified: a caller that appends
+ *                adds 1 to all lengths once all layers of the step are done.
+ *   k_new, v_new device, [B, Hkv, dh] of `dtype`, or both NULL: the new token's own row.  It is written at row len[b] of the
+ *                cache and attended to.  A video whose cache is full (or whose page for that row is not a page of the pool)
+ *                attends to it all the same, but it is not stored.
+ *   scale        > 0 and finite: s_j = scale * (q . k_j); usually 1 / sqrt(dh).
+ *   logit_cap    0: none.  c > 0: s_j becomes c * tanh(s_j / c).
+ *   out          device out, [B, Hq, dh] of `dtype`: sum_j p_j v_j with p = softmax(s) over the video's rows, accumulated in
+ *                fp32 and rounded once.  A video without rows gets zeros.
+ *   lse          device out, [B, Hq] float, or NULL: log sum_j exp(s_j) (-inf without rows), what two such results are joined by.
+ *   weight       device in/out, [B, weight_stride] float, or NULL: weight[b][j] grows by the mean of p_j over the Hq heads for
+ *                every row j that was there before; that of the appended row is set, not added to.  Entries behind the last row are left as
+ *                they were.  weight_stride >= the capacity.
+ *   Limits: dh in {32, 64, 128, 256} for bf16, {32, 64, 128} for f32; Hq a multiple of Hkv; 1 <= B <= METOK_MAX_DECODE_BATCH;
+ *   Hq <= 1024; capacity below 2^31 - 64; B * Hkv * ceil(Hq / Hkv / 16) and B * (capacity / 16 + 2) below 2^31.
+ *   out, lse and weight must not overlap anything else the call reads or writes.
+ *   workspace    metok_decode_attention_workspace_bytes(), S_cap being the capacity (pages_per_seq * page_size of a paged cache) and
+ *                with_weight whether `weight` is given.  Its contents on entry do not matter.
+ * ------------------------------------------------------------------------------------------- */
+METOK_API size_t metok_decode_attention_workspace_bytes(int B, int Hq, int Hkv, int64_t S_cap, int dh, int dtype, int with_weight);
+
+METOK_API int metok_decode_attention(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
+                           void* k_cache, void* v_cache, int64_t S_cap, const int32_t* len,
+                           const void* k_new, const void* v_new, double scale, double logit_cap,
+                           void* out, float* lse, float* weight, int64_t weight_stride,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same over a paged cache: k_pool, v_pool [n_pages_pool, Hkv, page_size, dh]; row j of video b is slot j % page_size of page
+ * page_table[b][j / page_size] (page_table device, [B, pages_per_seq] int32, as in metok_kv_compact_paged; after
+ * metok_kv_relink_paged the layer's own [B, pages_per_seq] part of page_table_out).  Entries outside [0, n_pages_pool) are never
+ * dereferenced: the rows behind them take no part.  Pages may be shared between videos as long as none of the appended rows
+ * lies in a shared page.  n_pages_pool * Hkv * page_size must be below 2^31.
+ */
+METOK_API int metok_decode_attention_paged(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
+                           void* k_pool, void* v_pool, int64_t n_pages_pool, int page_size,
+                           const int32_t* page_table, int pages_per_seq, const int32_t* len,
+                           const void* k_new, const void* v_new, double scale, double logit_cap,
+                           void* out, float* lse, float* weight, int64_t weight_stride,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* METOK_DECODE_H */

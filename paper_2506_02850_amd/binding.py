@@ -41,6 +41,10 @@ EXPORTS = [
     "metok_kv_compact_workspace_bytes", "metok_debug_set_move_spin_limit", "metok_trace_kernel",
     "metok_kv_relink_paged_workspace_bytes", "metok_kv_relink_paged",
 ]
+# those of metok_decode.h
+DECODE_EXPORTS = [
+    "metok_decode_attention_workspace_bytes", "metok_decode_attention", "metok_decode_attention_paged",
+]
 
 
 class AccountStruct(ctypes.Structure):
@@ -136,6 +140,13 @@ def _load() -> ctypes.CDLL:
     lib.metok_static_scratch_bytes.argtypes = []
     lib.metok_prefill_prune_static.restype = i32
     lib.metok_prefill_prune_static.argtypes = lib.metok_prefill_prune.argtypes[:-3] + [vp]
+    lib.metok_decode_attention_workspace_bytes.restype = sz
+    lib.metok_decode_attention_workspace_bytes.argtypes = [i32, i32, i32, i64, i32, i32, i32]
+    attend_tail = [vp, vp, vp, dbl, dbl, vp, vp, vp, i64, vp, sz, vp]
+    lib.metok_decode_attention.restype = i32
+    lib.metok_decode_attention.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, i64] + attend_tail
+    lib.metok_decode_attention_paged.restype = i32
+    lib.metok_decode_attention_paged.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, i64, i32, vp, i32] + attend_tail
     return lib
 
 
@@ -709,6 +720,87 @@ def metok_kv_relink_paged(k_pools: Sequence[torch.Tensor], v_pools: Sequence[tor
                                       _dev(ws, "workspace"), ws.numel(), _stream()))
     out["workspace"] = ws
     return out
+
+
+def _on_current_device(**tensors: Optional[torch.Tensor]) -> None:
+    """The library launches on the current device and its current stream: every tensor of a call lives there."""
+    here = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.is_cuda and t.device.index != here:
+            raise ValueError(f"{name} is on cuda:{t.device.index}, the current device is cuda:{here}")
+
+
+def _shaped(t: torch.Tensor, name: str, dtype: torch.dtype, shape) -> torch.Tensor:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t
+
+
+def metok_decode_attention_workspace_bytes(B: int, Hq: int, Hkv: int, S_cap: int, dh: int, dtype_code: int, with_weight: bool = False) -> int:
+    return int(_lib.metok_decode_attention_workspace_bytes(int(B), int(Hq), int(Hkv), int(S_cap), int(dh), int(dtype_code), int(bool(with_weight))))
+
+
+def _decode_attention(q, k, v, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out) -> Dict[str, torch.Tensor]:
+    _dev(q, "q")
+    if q.dim() != 3 or k.dim() != 4 or k.shape != v.shape:
+        raise ValueError("q must be [B, Hq, dh], K and V of one 4-dimensional shape")
+    B, Hq, dh = q.shape
+    dt, dev = _dtype_code(q), q.device
+    if page_table is None:
+        Hkv, S_cap = int(k.shape[1]), int(k.shape[2])
+        _shaped(k, "k_cache", q.dtype, (B, Hkv, S_cap, dh))
+    else:
+        n_pages, Hkv, page_size = (int(x) for x in k.shape[:3])
+        _shaped(k, "k_pool", q.dtype, (n_pages, Hkv, page_size, dh))
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [B, pages_per_seq]")
+        pages_per_seq = int(page_table.shape[1])
+        _shaped(page_table, "page_table", torch.int32, (B, pages_per_seq))
+        S_cap = pages_per_seq * page_size
+    _shaped(v, "V", q.dtype, k.shape)
+    _shaped(lens, "lens", torch.int32, (B,))
+    if (k_new is None) != (v_new is None):
+        raise ValueError("k_new and v_new go together")
+    if k_new is not None:
+        _shaped(k_new, "k_new", q.dtype, (B, Hkv, dh))
+        _shaped(v_new, "v_new", q.dtype, (B, Hkv, dh))
+    if weight is not None and (weight.dtype != torch.float32 or weight.dim() != 2 or weight.shape[0] != B):
+        raise ValueError("weight must be float32 [B, at least the capacity]")
+    _on_current_device(q=q, K=k, V=v, page_table=page_table, lens=lens, k_new=k_new, v_new=v_new, weight=weight, workspace=workspace,
+                       **{f"out[{n!r}]": t for n, t in (out or {}).items()})
+    result = dict(out=_out(out, "out", (B, Hq, dh), q.dtype, dev), lse=_out(out, "lse", (B, Hq), torch.float32, dev))
+    ws = workspace if workspace is not None else _workspace(
+        _lib.metok_decode_attention_workspace_bytes(B, Hq, Hkv, S_cap, dh, dt, int(weight is not None)), dev)
+    scale = dh ** -0.5 if scale is None else float(scale)
+    tail = (_dev(lens, "lens"), _dev(k_new, "k_new"), _dev(v_new, "v_new"), scale, float(logit_cap), _dev(result["out"], "out"), _dev(result["lse"], "lse"),
+            _dev(weight, "weight"), weight.shape[1] if weight is not None else 0, _dev(ws, "workspace"), ws.numel() * ws.element_size(), _stream())
+    if page_table is None:
+        _check(_lib.metok_decode_attention(_dev(q, "q"), B, Hq, Hkv, dh, dt, _dev(k, "k_cache"), _dev(v, "v_cache"), S_cap, *tail))
+    else:
+        _check(_lib.metok_decode_attention_paged(_dev(q, "q"), B, Hq, Hkv, dh, dt, _dev(k, "k_pool"), _dev(v, "v_pool"), n_pages, page_size,
+                                                 _dev(page_table, "page_table"), pages_per_seq, *tail))
+    return result
+
+
+def metok_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, lens: torch.Tensor,
+                           k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                           scale: Optional[float] = None, logit_cap: float = 0.0, weight: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """Attention of one new token per video, q [B, Hq, dh], over the first lens[b] rows of one layer's cache [B, Hkv, S_cap, dh].
+    k_new / v_new [B, Hkv, dh]: the token's own row, stored at row lens[b] and attended to (lens is not changed).  weight [B, >= S_cap]
+    float32 grows by every row's attention weight, averaged over the query heads.  scale defaults to dh ** -0.5.  Returns out [B, Hq, dh]
+    and lse [B, Hq]; `out` may carry preallocated tensors under these names."""
+    return _decode_attention(q, k_cache, v_cache, None, lens, k_new, v_new, scale, logit_cap, weight, workspace, out)
+
+
+def metok_decode_attention_paged(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor,
+                                 k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                                 scale: Optional[float] = None, logit_cap: float = 0.0, weight: Optional[torch.Tensor] = None,
+                                 workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """metok_decode_attention over one layer's pools [n_pages, Hkv, page_size, dh] through page_table [B, pages_per_seq]."""
+    if page_table is None:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    return _decode_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out)
 
 
 def metok_debug_set_move_spin_limit(polls: int) -> None:

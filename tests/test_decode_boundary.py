@@ -1,0 +1,169 @@
+"""CPU checks of the decoding-time calls: exports, workspace sizes, refusals before anything reaches a GPU, the split's plan."""
+import ctypes
+import os
+import random
+import re
+
+import pytest
+import torch  # noqa: F401  (loaded first so that the library binds to the same HIP runtime)
+
+from tests.host_plan import host_library
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "metok_decode.h")
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2506_02850_amd import build
+    if not os.path.exists(build.LIB):
+        build.build(verbose=False)
+    from paper_2506_02850_amd import binding
+    return binding
+
+
+def test_every_declared_symbol_is_exported_and_bound(B):
+    names = re.findall(r"METOK_API\s+[\w\s\*]+?\b(metok_\w+)\s*\(", open(HEADER).read())
+    assert len(set(names)) == len(names) and sorted(names) == sorted(B.DECODE_EXPORTS)
+    for name in names:
+        assert hasattr(B.lib(), name) and callable(getattr(B, name)), name
+
+
+def test_header_is_plain_c(tmp_path):
+    import subprocess
+    src = tmp_path / "x.c"
+    src.write_text('#include "metok_decode.h"\nint main(void) { return METOK_MAX_DECODE_BATCH == 4096 ? 0 : 1; }\n')
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-c", str(src), "-o", str(tmp_path / "x.o")], check=True)
+
+
+FAKE = [0x10000000 * (i + 1) for i in range(16)]        # aligned, far apart, never dereferenced: validation fails first
+
+
+def attention_args(**kw):
+    a = dict(q=FAKE[0], B=2, Hq=8, Hkv=2, dh=64, dtype=1, k=FAKE[1], v=FAKE[2], S_cap=128, len=FAKE[3], k_new=FAKE[4], v_new=FAKE[5], scale=0.125,
+             cap=0.0, out=FAKE[6], lse=FAKE[7], weight=FAKE[8], stride=128, ws=FAKE[9], bytes=0, stream=None)
+    a.update(kw)
+    return list(a.values())
+
+
+def test_refused_attention_calls(B):
+    f = B.lib().metok_decode_attention
+
+    def refused(code, text, **kw):
+        assert f(*attention_args(**kw)) == code, kw
+        assert text in B.metok_last_error(), (kw, B.metok_last_error())
+
+    refused(-3, "workspace")
+    refused(-3, "workspace", ws=None, bytes=1 << 30)
+    refused(-3, "workspace", ws=FAKE[9] + 8, bytes=1 << 30)
+    for name in ("q", "k", "v", "len", "out"):
+        refused(-1, "NULL", **{name: None})
+    refused(-1, "go together", k_new=None)
+    refused(-1, "go together", v_new=None)
+    for name in ("q", "k", "v", "k_new", "v_new", "out"):
+        refused(-1, "aligned", **{name: FAKE[10] + 8})
+    for name in ("len", "lse", "weight"):
+        refused(-1, "aligned", **{name: FAKE[10] + 2})
+    for scale in (0.0, -1.0, float("nan"), float("inf")):
+        refused(-1, "scale", scale=scale)
+    for cap in (-1.0, float("nan"), float("inf")):
+        refused(-1, "logit_cap", cap=cap)
+    refused(-1, "weight_stride", stride=127)
+    refused(-1, "dtype", dtype=2)
+    for n in (0, -1, 4097):
+        refused(-1, "B must", B=n)
+    for hq, hkv in ((8, 3), (0, 2), (8, 0), (7, 2), (1025, 1), (-8, -2)):
+        refused(-1, "Hq must", Hq=hq, Hkv=hkv)
+    for dh in (0, 16, 96, 512):
+        refused(-1, "dh must", dh=dh)
+    refused(-1, "dh must", dh=256, dtype=0)
+    for s in (0, -5, 2 ** 31 - 64, 2 ** 40):
+        refused(-1, "capacity", S_cap=s, stride=2 ** 41)
+    refused(-1, "too many rows", B=4096, S_cap=2 ** 30, stride=2 ** 41)
+    big = 1 << 40
+    refused(-1, "overlaps", out=FAKE[0], bytes=big)
+    refused(-1, "overlaps", lse=FAKE[6], bytes=big)
+    refused(-1, "overlaps", v=FAKE[1], bytes=big)
+    refused(-1, "overlaps", v=FAKE[1] + 16, bytes=big)
+    refused(-1, "overlaps", k_new=FAKE[1] + 64, bytes=big)
+    refused(-1, "overlaps", weight=FAKE[3], bytes=big)
+    refused(-1, "overlaps", ws=FAKE[2], bytes=big)
+
+
+def test_refused_paged_attention_calls(B):
+    f = B.lib().metok_decode_attention_paged
+
+    def refused(code, text, **kw):
+        a = dict(q=FAKE[0], B=2, Hq=8, Hkv=2, dh=64, dtype=1, k=FAKE[1], v=FAKE[2], n_pages=20, page=16, table=FAKE[11], pps=8, len=FAKE[3], k_new=None, v_new=None,
+                 scale=0.125, cap=0.0, out=FAKE[6], lse=None, weight=None, stride=0, ws=FAKE[9], bytes=0, stream=None)
+        a.update(kw)
+        assert f(*a.values()) == code, kw
+        assert text in B.metok_last_error(), (kw, B.metok_last_error())
+
+    refused(-3, "workspace", pps=80)
+    refused(-1, "page_table", table=None)
+    refused(-1, "page_table", table=FAKE[11] + 1)
+    for name in ("n_pages", "page", "pps"):
+        refused(-1, "positive", **{name: 0})
+    refused(-1, "capacity", page=2 ** 20, pps=2 ** 20)
+    refused(-2, "below 2^31", n_pages=2 ** 40, pps=80)
+    refused(-2, "below 2^31", n_pages=2 ** 31 // 32 + 1, pps=80)
+    refused(-1, "overlaps", table=FAKE[1], bytes=1 << 40)
+
+
+def test_workspace_sizes(B):
+    f = B.metok_decode_attention_workspace_bytes
+    assert f(1, 28, 4, 100, 128, B.BF16) == 0                           # one workgroup per kv head: nothing to join
+    small, big = f(8, 28, 4, 36992, 128, B.BF16), f(8, 28, 4, 36992, 128, B.BF16, True)
+    assert 0 < small < 16 << 20
+    assert big - small >= 8 * 28 * 36993 * 4                            # the logits
+    assert f(8, 28, 4, 36992, 128, B.F32) > 0
+    for bad in ((0, 28, 4, 100, 128, 1), (1, 28, 5, 100, 128, 1), (1, 28, 4, 0, 128, 1), (1, 28, 4, 100, 48, 1), (1, 28, 4, 100, 256, 0), (1, 28, 4, 100, 128, 7)):
+        assert f(*bad) == 0
+
+
+PLAN = r"""
+#include "decode_plan.h"
+using namespace metok;
+extern "C" void attend_plan(int B, int Hq, int Hkv, int64_t cap, int dh, int esize, int w, int64_t* o) {
+    const AttendPlan p = plan_attend(B, Hq, Hkv, cap, dh, esize, w != 0);
+    for (int64_t v : {int64_t(p.tile), int64_t(p.row_blocks), int64_t(p.rows), p.pairs, p.grid, int64_t(p.joined), p.logit_stride, int64_t(p.part_ml),
+                      int64_t(p.part_o), int64_t(p.lse2), int64_t(p.logits), int64_t(p.bytes)}) *o++ = v;
+}
+extern "C" int64_t tiles_per_group(int64_t t) { return attend_tiles_per_group(t); }
+"""
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_the_grid_holds_every_share(seed):
+    """Whatever the lengths: the workgroups that the videos' rows ask for are at most the grid, a call that is not joined has one per
+    pair, and the parts of the workspace lie one behind the other."""
+    lib = host_library("#include <initializer_list>\n" + PLAN)
+    lib.tiles_per_group.restype = ctypes.c_int64
+    rng = random.Random(seed)
+    for _ in range(400):
+        Hq, Hkv = rng.choice([(28, 4), (40, 40), (71, 1), (17, 1), (8, 8), (1, 1), (1024, 2)])
+        Bn = rng.choice([1, 2, 8, 64, 65, 500, 4096])
+        esize, dh = rng.choice([(2, 128), (4, 64), (2, 256)])
+        cap = int(2 ** rng.uniform(0, 18))
+        w = rng.randint(0, 1)
+        o = (ctypes.c_int64 * 12)()
+        lib.attend_plan(Bn, Hq, Hkv, ctypes.c_int64(cap), dh, esize, w, o)
+        tile, row_blocks, rows, pairs, grid, joined, stride, ml, part, lse2, logits, total = list(o)
+        heads = Hkv * row_blocks
+        assert pairs == Bn * heads and row_blocks * 16 >= Hq // Hkv > (row_blocks - 1) * 16
+        for kind in range(4):
+            fresh = rng.randint(0, 1)
+            lens = [cap if kind == 0 else (0 if kind == 1 else rng.randint(0, cap) if kind == 2 or rng.random() < 0.02 else min(cap, 3)) for _ in range(Bn)]
+            tiles = [-(-(n + fresh) // tile) for n in lens]
+            per = lib.tiles_per_group(ctypes.c_int64(sum(tiles) * heads))
+            splits = [max(1, -(-t // per)) for t in tiles]
+            assert sum(splits) * heads <= grid
+            assert joined or max(splits) == 1
+            assert all(s <= max(t, 1) for s, t in zip(splits, tiles))
+        if joined:
+            assert part - ml >= grid * rows * 2 * 4 and lse2 - part >= grid * rows * dh * 4
+        if w:
+            assert stride >= cap + 1 and stride % 32 == 0 and logits - lse2 >= Bn * Hq * 4 and total - logits == -(-Bn * Hq * stride * 4 // 256) * 256
+        else:
+            assert logits == total
