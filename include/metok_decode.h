@@ -2,9 +2,10 @@
  * metok_decode.h -- C ABI of the decoding-time operators beside stage 3 (AMD MI355X, gfx950).
  *
  * Stage 3 of METok (arXiv 2506.02850, Sec. 3.3) leaves a compacted KV cache (Eq. 3); while the answer is written, every new token
- * attends to it and adds a row:
+ * attends to it and adds a row.  Two operators belong to that loop:
  *   - the attention of one new token per video over a dense or paged cache, which appends the token's own row and, if asked,
- *     adds up how much attention every cached row draws (the decoding-time counterpart of the stage-2 score, Sec. 3.2.2).
+ *     adds up how much attention every cached row draws (the decoding-time counterpart of the stage-2 score, Sec. 3.2.2);
+ *   - eviction: once a cache has grown beyond a budget, the rows that drew the least attention leave it.
  * The conventions of metok.h hold (caller-owned buffers, no synchronisation, deterministic results, capture into HIP graphs after
  * one ordinary call, error codes, 16-byte alignment, finite inputs).  Two additions:
  *   - Lengths live on the device, so that a captured decoding step can be replayed while the caches grow.  A length below 0 counts
@@ -68,6 +69,49 @@ METOK_API int metok_decode_attention_paged(const void* q, int B, int Hq, int Hkv
                            const void* k_new, const void* v_new, double scale, double logit_cap,
                            void* out, float* lse, float* weight, int64_t weight_stride,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Eviction by accumulated attention weight: every (layer, video) whose cache holds more rows than the layer's budget keeps its
+ * first n_first rows, its last n_last rows and, of those between, the rows with the largest weight (the lower index first among
+ * equals) until the budget is full.  Rows keep their order (as in stage 3), so a row's rank tells its age.
+ *
+ *   k_layers, v_layers, L, B, Hkv, S_cap, dh, dtype  the caches, as in metok_kv_compact.
+ *   weight       host array of L device pointers, weight[l] [B, weight_stride] float (see `weight` above; weight_stride >= the
+ *                capacity); weight[l] == NULL leaves layer l alone.  Weights are compared as numbers; NaNs come at the ends by sign.
+ *   weight_out   host array of L device pointers like `weight`: weight_out[l][b][i] = weight of the row that is now row i, for
+ *                i < new_len[l][b]; the rest is left as it was.  May be the same buffers as `weight` (or the same array), but not
+ *                overlap them otherwise.
+ *   len          device, [L, B] int32: rows held now.
+ *   budget       host, [L] int32, 1 <= budget[l] <= capacity (ignored where weight[l] is NULL); n_first, n_last >= 0 and
+ *                n_first + n_last <= budget[l].
+ *   idx          host array of L device pointers, idx[l] [B, budget[l]] int32 out (ignored where weight[l] is NULL): the kept rows, ascending -- the
+ *                index lists of metok_kv_compact, _paged and metok_kv_relink_paged with n_keep[l] = budget[l].  A video within the budget has
+ *                the list 0, 1, 2, ...: nothing of it moves.
+ *   new_len      device out, [L, B] int32: min(len, budget[l]) (len where weight[l] is NULL); may be `len` itself.
+ * metok_kv_evict and metok_kv_evict_paged select and move the rows of the caches (row i <- row idx[l][b][i]; rows from
+ * new_len on are left as they were); metok_kv_evict_select only selects, for callers that relink pages or move the rows themselves.
+ *   workspace    metok_kv_evict_workspace_bytes() for the first two, none for the selection; as in metok_kv_compact its first word
+ *                is 0 after the call unless a bounded wait expired.
+ * ------------------------------------------------------------------------------------------- */
+METOK_API size_t metok_kv_evict_workspace_bytes(int L, int B, int Hkv, int64_t S_cap, int dh, int dtype);
+
+METOK_API int metok_kv_evict(void* const* k_layers, void* const* v_layers, int L, int B, int Hkv, int64_t S_cap, int dh, int dtype,
+                           const float* const* weight, float* const* weight_out, int64_t weight_stride,
+                           const int32_t* len, const int32_t* budget, int n_first, int n_last,
+                           int32_t* const* idx, int32_t* new_len,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+METOK_API int metok_kv_evict_paged(void* const* k_pools, void* const* v_pools, int L, int B, int Hkv,
+                           int64_t n_pages_pool, int page_size, int dh, int dtype,
+                           const int32_t* page_table, int pages_per_seq,
+                           const float* const* weight, float* const* weight_out, int64_t weight_stride,
+                           const int32_t* len, const int32_t* budget, int n_first, int n_last,
+                           int32_t* const* idx, int32_t* new_len,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+METOK_API int metok_kv_evict_select(const float* const* weight, float* const* weight_out, int64_t weight_stride,
+                           int L, int B, int64_t S_cap, const int32_t* len, const int32_t* budget, int n_first, int n_last,
+                           int32_t* const* idx, int32_t* new_len, void* stream);
 
 #ifdef __cplusplus
 }

@@ -44,6 +44,7 @@ EXPORTS = [
 # those of metok_decode.h
 DECODE_EXPORTS = [
     "metok_decode_attention_workspace_bytes", "metok_decode_attention", "metok_decode_attention_paged",
+    "metok_kv_evict_workspace_bytes", "metok_kv_evict", "metok_kv_evict_paged", "metok_kv_evict_select",
 ]
 
 
@@ -147,6 +148,16 @@ def _load() -> ctypes.CDLL:
     lib.metok_decode_attention.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, i64] + attend_tail
     lib.metok_decode_attention_paged.restype = i32
     lib.metok_decode_attention_paged.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, i64, i32, vp, i32] + attend_tail
+    lib.metok_kv_evict_workspace_bytes.restype = sz
+    lib.metok_kv_evict_workspace_bytes.argtypes = [i32, i32, i32, i64, i32, i32]
+    vpp, ints = c.POINTER(vp), c.POINTER(c.c_int32)
+    select_tail = [vp, ints, i32, i32, vpp, vp]
+    lib.metok_kv_evict.restype = i32
+    lib.metok_kv_evict.argtypes = [vpp, vpp, i32, i32, i32, i64, i32, i32, vpp, vpp, i64] + select_tail + [vp, sz, vp]
+    lib.metok_kv_evict_paged.restype = i32
+    lib.metok_kv_evict_paged.argtypes = [vpp, vpp, i32, i32, i32, i64, i32, i32, i32, vp, i32, vpp, vpp, i64] + select_tail + [vp, sz, vp]
+    lib.metok_kv_evict_select.restype = i32
+    lib.metok_kv_evict_select.argtypes = [vpp, vpp, i64, i32, i32, i64] + select_tail + [vp]
     return lib
 
 
@@ -801,6 +812,129 @@ def metok_decode_attention_paged(q: torch.Tensor, k_pool: torch.Tensor, v_pool: 
     if page_table is None:
         raise ValueError("page_table must be int32 [B, pages_per_seq]")
     return _decode_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out)
+
+
+def metok_kv_evict_workspace_bytes(L: int, B: int, Hkv: int, S_cap: int, dh: int, dtype_code: int) -> int:
+    return int(_lib.metok_kv_evict_workspace_bytes(int(L), int(B), int(Hkv), int(S_cap), int(dh), int(dtype_code)))
+
+
+class _Eviction:
+    """The arguments that the three eviction calls share: checked, outputs made, pointers laid out."""
+
+    def __init__(self, weight, lens, budget, weight_out, idx, new_len):
+        L = self.L = len(weight)
+        given = [w for w in weight if w is not None]
+        if not given:
+            raise ValueError("weight: at least one layer must be given")
+        first = given[0]
+        if first.dim() != 2:
+            raise ValueError("weight[l] must be float32 [B, at least the capacity]")
+        B, W = self.B, self.W = tuple(first.shape)
+        for w in given:
+            _shaped(w, "weight[l]", torch.float32, (B, W))
+        _shaped(lens, "lens", torch.int32, (L, B))
+        self.budget = [int(budget)] * L if isinstance(budget, int) else [int(x) for x in budget]
+        if len(self.budget) != L:
+            raise ValueError("budget must be one number or one per layer")
+        if weight_out is None:
+            weight_out = weight
+        if len(weight_out) != L or (idx is not None and len(idx) != L):
+            raise ValueError("weight, weight_out and idx must have one entry per layer")
+        dev = first.device
+        self.weight_out, self.idx = list(weight_out), []
+        for l, w in enumerate(weight):
+            if w is None:
+                self.idx.append(None)
+                continue
+            if self.weight_out[l] is None:
+                raise ValueError("weight_out must be given where weight is")
+            _shaped(self.weight_out[l], "weight_out[l]", torch.float32, (B, W))
+            shape = (B, max(self.budget[l], 0))
+            self.idx.append(_shaped(idx[l], "idx[l]", torch.int32, shape) if idx is not None and idx[l] is not None
+                            else torch.empty(shape, dtype=torch.int32, device=dev))
+        self.new_len = torch.empty((L, B), dtype=torch.int32, device=dev) if new_len is None else _shaped(new_len, "new_len", torch.int32, (L, B))
+        self.device, self.lens = dev, lens
+        for name, tensors in (("weight", weight), ("weight_out", self.weight_out), ("idx", self.idx), ("lens", [lens]), ("new_len", [self.new_len])):
+            for t in tensors:
+                if t is not None:
+                    _dev(t, name)
+                    _on_current_device(**{name: t})
+        vp = ctypes.c_void_p
+
+        def pointers(tensors):
+            return (vp * L)(*[t.data_ptr() if t is not None and weight[l] is not None else None for l, t in enumerate(tensors)])
+
+        self.weights = (pointers(weight), pointers(self.weight_out), W)
+        self.lengths = (lens.data_ptr(), (ctypes.c_int32 * L)(*self.budget))
+        self.outputs = (pointers(self.idx), self.new_len.data_ptr())
+
+    def result(self) -> Dict[str, object]:
+        return dict(idx=self.idx, new_len=self.new_len, weight=self.weight_out)
+
+
+def _kv_evict(k_layers, v_layers, page_table, weight, lens, budget, n_first, n_last, weight_out, idx, new_len, workspace):
+    e = _Eviction(weight, lens, budget, weight_out, idx, new_len)
+    if len(k_layers) != e.L or len(v_layers) != e.L:
+        raise ValueError("K buffers, V buffers and weight must have one entry per layer")
+    shape, dt = tuple(k_layers[0].shape), _dtype_code(k_layers[0])
+    if len(shape) != 4:
+        raise ValueError("K and V must be 4-dimensional")
+    if page_table is None:
+        B, Hkv, S_cap, dh = shape
+        if B != e.B:
+            raise ValueError(f"the caches hold {B} videos, weight {e.B}")
+    else:
+        n_pages, Hkv, page_size, dh = shape
+        if page_table.dim() != 2:
+            raise ValueError("page_table must be int32 [B, pages_per_seq]")
+        pages_per_seq = int(page_table.shape[1])
+        _shaped(page_table, "page_table", torch.int32, (e.B, pages_per_seq))
+        S_cap = pages_per_seq * page_size
+    for name, layers in (("K", k_layers), ("V", v_layers)):
+        for t in layers:
+            _shaped(t, name, k_layers[0].dtype, shape)
+            _on_current_device(**{name: t})
+    _on_current_device(page_table=page_table, workspace=workspace)
+    vp = ctypes.c_void_p
+    karr, varr = ((vp * e.L)(*[_dev(t, name) for t in layers]) for name, layers in (("K buffer", k_layers), ("V buffer", v_layers)))
+    ws = workspace if workspace is not None else _workspace(_lib.metok_kv_evict_workspace_bytes(e.L, e.B, Hkv, S_cap, dh, dt), e.device)
+    tail = (*e.weights, *e.lengths, int(n_first), int(n_last), *e.outputs, _dev(ws, "workspace"), ws.numel() * ws.element_size(), _stream())
+    if page_table is None:
+        _check(_lib.metok_kv_evict(karr, varr, e.L, e.B, Hkv, S_cap, dh, dt, *tail))
+    else:
+        _check(_lib.metok_kv_evict_paged(karr, varr, e.L, e.B, Hkv, n_pages, page_size, dh, dt, _dev(page_table, "page_table"), pages_per_seq, *tail))
+    return e.result()
+
+
+def metok_kv_evict(k_layers: Sequence[torch.Tensor], v_layers: Sequence[torch.Tensor], weight: Sequence[Optional[torch.Tensor]],
+                   lens: torch.Tensor, budget, n_first: int = 0, n_last: int = 0,
+                   weight_out: Optional[Sequence[Optional[torch.Tensor]]] = None, idx: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                   new_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> Dict[str, object]:
+    """Shrinks every video's cache to `budget` rows (one number, or one per layer) in every layer: the first n_first, the last n_last and the
+    rows between with the largest weight stay, in order.  k_layers / v_layers [B, Hkv, S_cap, dh], weight[l] [B, >= S_cap] float32 as
+    metok_decode_attention accumulates it (None: layer left alone), lens [L, B] int32.  Weights move along, in place unless weight_out is
+    given.  Returns idx (per layer [B, budget], the lists of metok_kv_compact), new_len [L, B] and weight; nothing is synchronised."""
+    return _kv_evict(k_layers, v_layers, None, weight, lens, budget, n_first, n_last, weight_out, idx, new_len, workspace)
+
+
+def metok_kv_evict_paged(k_pools: Sequence[torch.Tensor], v_pools: Sequence[torch.Tensor], page_table: torch.Tensor,
+                         weight: Sequence[Optional[torch.Tensor]], lens: torch.Tensor, budget, n_first: int = 0, n_last: int = 0,
+                         weight_out: Optional[Sequence[Optional[torch.Tensor]]] = None, idx: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                         new_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> Dict[str, object]:
+    """metok_kv_evict on paged pools [n_pages, Hkv, page_size, dh] through page_table [B, pages_per_seq], shared by the layers."""
+    if page_table is None:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    return _kv_evict(k_pools, v_pools, page_table, weight, lens, budget, n_first, n_last, weight_out, idx, new_len, workspace)
+
+
+def metok_kv_evict_select(weight: Sequence[Optional[torch.Tensor]], lens: torch.Tensor, S_cap: int, budget, n_first: int = 0, n_last: int = 0,
+                          weight_out: Optional[Sequence[Optional[torch.Tensor]]] = None, idx: Optional[Sequence[Optional[torch.Tensor]]] = None,
+                          new_len: Optional[torch.Tensor] = None) -> Dict[str, object]:
+    """The selection of metok_kv_evict alone, for caches of capacity S_cap whose rows the caller moves, or whose pages it relinks
+    (metok_kv_relink_paged with these index lists)."""
+    e = _Eviction(weight, lens, budget, weight_out, idx, new_len)
+    _check(_lib.metok_kv_evict_select(*e.weights, e.L, e.B, int(S_cap), *e.lengths, int(n_first), int(n_last), *e.outputs, _stream()))
+    return e.result()
 
 
 def metok_debug_set_move_spin_limit(polls: int) -> None:

@@ -85,10 +85,17 @@ struct LengthTable { int n; int32_t len[METOK_MAX_LAYERS]; };
 
 RowMoveGeom row_move_geom(int64_t row_bytes);
 size_t row_move_workspace_bytes(int L, int B, int Hkv, int n_which, int64_t S_cap, int64_t row_bytes);
+// A launch that takes the place of the mover's own first one: it clears the words before the moves and may write the index lists.
+struct RowMoveStart { int (*launch)(void* context, uint32_t* words, size_t n_words, hipStream_t st); void* context; };
 int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_which, int64_t S_cap, int64_t row_bytes,
                      const int32_t* page_table, int page_size, int pages_per_seq, int64_t n_pages_pool,
                      int32_t* new_len, const int32_t* host_len, int L_total,
-                     void* workspace, size_t workspace_bytes, hipStream_t st, const RelinkTables* relink);
+                     void* workspace, size_t workspace_bytes, hipStream_t st, const RelinkTables* relink, const RowMoveStart* start = nullptr);
+// metok_kv_compact (page_table NULL) and metok_kv_compact_paged (S_cap = pages_per_seq * page_size).
+int compact_layers(void* const* k_layers, void* const* v_layers, int L, int B, int Hkv, int64_t S_cap, int dh, int dtype,
+                   const int32_t* const* idx, const int32_t* n_keep, int32_t* new_len,
+                   const int32_t* page_table, int page_size, int pages_per_seq, int64_t n_pages_pool,
+                   void* workspace, size_t workspace_bytes, void* stream, const RowMoveStart* start = nullptr);
 
 // ---------------------------------------------------------------------------------------------
 // device helpers

@@ -476,7 +476,7 @@ size_t row_move_workspace_bytes(int L, int B, int Hkv, int n_which, int64_t S_ca
 int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_which, int64_t S_cap, int64_t row_bytes,
                      const int32_t* page_table, int page_size, int pages_per_seq, int64_t n_pages_pool,
                      int32_t* new_len, const int32_t* host_len, int L_total,
-                     void* workspace, size_t workspace_bytes, hipStream_t st, const RelinkTables* relink) {
+                     void* workspace, size_t workspace_bytes, hipStream_t st, const RelinkTables* relink, const RowMoveStart* start) {
     const RowMoveGeom g = row_move_geom(row_bytes);
     const size_t need = row_move_workspace_bytes(L_total, B, Hkv, n_which, S_cap, row_bytes);
     if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15u))
@@ -486,17 +486,6 @@ int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_w
     const int n_sub = Hkv * n_which * g.parts;
     const int tiles_max = static_cast<int>((S_cap + g.rows_per_tile - 1) / g.rows_per_tile);
     const size_t used_words = header + static_cast<size_t>(n_active) * B * n_sub * tiles_max;
-
-    // one small launch clears the flags / tickets / error word and writes the lengths (L_total <= METOK_MAX_LAYERS)
-    LengthTable lengths;
-    lengths.n = new_len ? L_total : 0;
-    for (int l = 0; l < lengths.n; ++l) lengths.len[l] = host_len[l];
-    unsigned init_blocks = static_cast<unsigned>((used_words + 1023) / 1024);
-    if (init_blocks < 1) init_blocks = 1;
-    if (init_blocks > 1024) init_blocks = 1024;
-    hipLaunchKernelGGL(move_init_kernel, dim3(init_blocks), dim3(256), 0, st, words, used_words, new_len, lengths);
-    int rc = check_launch("row move init");
-    if (rc) return rc;
 
     // the place of every layer in the launches
     const int n_launches = move_launches(L_total);
@@ -515,6 +504,21 @@ int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_w
         if (items > INT32_MAX) return fail(METOK_ERR_INVALID_ARG, "too many tiles for one launch");
         launch_items[launch] = items;
     }
+    // one small launch clears the flags / tickets / error word and writes the lengths (L_total <= METOK_MAX_LAYERS)
+    LengthTable lengths;
+    lengths.n = new_len ? L_total : 0;
+    for (int l = 0; l < lengths.n; ++l) lengths.len[l] = host_len[l];
+    unsigned init_blocks = static_cast<unsigned>((used_words + 1023) / 1024);
+    if (init_blocks < 1) init_blocks = 1;
+    if (init_blocks > 1024) init_blocks = 1024;
+    int rc;
+    if (start) rc = start->launch(start->context, words, used_words, st);
+    else {
+        hipLaunchKernelGGL(move_init_kernel, dim3(init_blocks), dim3(256), 0, st, words, used_words, new_len, lengths);
+        rc = check_launch("row move init");
+    }
+    if (rc) return rc;
+
     if (relink) {
         // the planning kernel runs between the clearing of the flags and the moves: it raises the flags of the tiles
         // that have nothing to copy and lists the others
@@ -568,11 +572,11 @@ int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_w
 using namespace metok;
 
 // Shared host path.  Dense: page_table == nullptr.  Paged: S_cap = pages_per_seq * page_size.
-static int compact_impl(void* const* k_layers, void* const* v_layers, int L, int B, int Hkv,
-                        int64_t S_cap, int dh, int dtype,
-                        const int32_t* const* idx, const int32_t* n_keep, int32_t* new_len,
-                        const int32_t* page_table, int page_size, int pages_per_seq, int64_t n_pages_pool,
-                        void* workspace, size_t workspace_bytes, void* stream) {
+int metok::compact_layers(void* const* k_layers, void* const* v_layers, int L, int B, int Hkv,
+                          int64_t S_cap, int dh, int dtype,
+                          const int32_t* const* idx, const int32_t* n_keep, int32_t* new_len,
+                          const int32_t* page_table, int page_size, int pages_per_seq, int64_t n_pages_pool,
+                          void* workspace, size_t workspace_bytes, void* stream, const RowMoveStart* start) {
     if (dtype != METOK_F32 && dtype != METOK_BF16) return fail(METOK_ERR_INVALID_ARG, "unknown dtype %d", dtype);
     if (L < 1 || L > METOK_MAX_LAYERS) return fail(METOK_ERR_INVALID_ARG, "L must be in [1, %d], got %d", METOK_MAX_LAYERS, L);
     if (B < 1 || Hkv < 1 || dh < 1 || S_cap < 1 || S_cap > INT32_MAX)
@@ -613,7 +617,7 @@ static int compact_impl(void* const* k_layers, void* const* v_layers, int L, int
     int32_t host_len[METOK_MAX_LAYERS];
     for (int l = 0; l < L; ++l) host_len[l] = idx[l] ? n_keep[l] : static_cast<int32_t>(S_cap);
     return launch_row_moves(layers, n_active, B, Hkv, 2, S_cap, row_bytes, page_table, page_size, pages_per_seq, n_pages_pool,
-                            new_len, host_len, L, workspace, workspace_bytes, static_cast<hipStream_t>(stream), nullptr);
+                            new_len, host_len, L, workspace, workspace_bytes, static_cast<hipStream_t>(stream), nullptr, start);
 }
 
 extern "C" size_t metok_kv_compact_workspace_bytes(int L, int B, int Hkv, int64_t S_cap, int dh, int dtype) {
@@ -630,8 +634,8 @@ extern "C" int metok_kv_compact(void* const* k_layers, void* const* v_layers, in
                                 const int32_t* const* idx, const int32_t* n_keep, int32_t* new_len,
                                 void* workspace, size_t workspace_bytes, void* stream) {
     clear_error();
-    return compact_impl(k_layers, v_layers, L, B, Hkv, S_cap, dh, dtype, idx, n_keep, new_len, nullptr, 0, 0, 0,
-                        workspace, workspace_bytes, stream);
+    return compact_layers(k_layers, v_layers, L, B, Hkv, S_cap, dh, dtype, idx, n_keep, new_len, nullptr, 0, 0, 0,
+                          workspace, workspace_bytes, stream);
 }
 
 extern "C" int metok_kv_compact_paged(void* const* k_pools, void* const* v_pools, int L, int B, int Hkv,
@@ -645,8 +649,8 @@ extern "C" int metok_kv_compact_paged(void* const* k_pools, void* const* v_pools
         return fail(METOK_ERR_INVALID_ARG, "page_size, pages_per_seq and n_pages_pool must be positive");
     const int64_t S_cap = static_cast<int64_t>(pages_per_seq) * page_size;
     if (S_cap > INT32_MAX) return fail(METOK_ERR_INVALID_ARG, "pages_per_seq * page_size must be below 2^31");
-    return compact_impl(k_pools, v_pools, L, B, Hkv, S_cap, dh, dtype, idx, n_keep, new_len, page_table, page_size, pages_per_seq,
-                        n_pages_pool, workspace, workspace_bytes, stream);
+    return compact_layers(k_pools, v_pools, L, B, Hkv, S_cap, dh, dtype, idx, n_keep, new_len, page_table, page_size, pages_per_seq,
+                          n_pages_pool, workspace, workspace_bytes, stream);
 }
 
 // Test hook: how often a tile polls one flag before it gives its wait up (default 2^24).  With 0 every

@@ -167,3 +167,101 @@ def test_the_grid_holds_every_share(seed):
             assert stride >= cap + 1 and stride % 32 == 0 and logits - lse2 >= Bn * Hq * 4 and total - logits == -(-Bn * Hq * stride * 4 // 256) * 256
         else:
             assert logits == total
+
+
+def evict_args(**kw):
+    vp, i32 = ctypes.c_void_p, ctypes.c_int32
+    a = dict(k=(vp * 2)(FAKE[0], FAKE[1]), v=(vp * 2)(FAKE[2], FAKE[3]), L=2, B=2, Hkv=2, S_cap=128, dh=64, dtype=1,
+             weight=(vp * 2)(FAKE[4], FAKE[5]), weight_out=(vp * 2)(FAKE[6], FAKE[7]), stride=128, len=FAKE[8], budget=(i32 * 2)(64, 64), first=4, last=8,
+             idx=(vp * 2)(FAKE[9], FAKE[10]), new_len=FAKE[11], ws=FAKE[12], bytes=0, stream=None)
+    a.update(kw)
+    return a
+
+
+def test_refused_evictions(B):
+    vp, i32 = ctypes.c_void_p, ctypes.c_int32
+
+    def refused(code, text, **kw):
+        a = evict_args(**kw)
+        assert B.lib().metok_kv_evict(*a.values()) == code, kw
+        assert text in B.metok_last_error(), (kw, B.metok_last_error())
+        if code == -1 and not {"k", "v", "dtype", "dh", "Hkv"} & set(kw):
+            b = [a[n] for n in ("weight", "weight_out", "stride", "L", "B", "S_cap", "len", "budget", "first", "last", "idx", "new_len", "stream")]
+            assert B.lib().metok_kv_evict_select(*b) == code and text in B.metok_last_error()
+
+    refused(-3, "workspace")
+    refused(-3, "workspace", ws=None, bytes=1 << 30)
+    for n in (0, -1, 129):
+        refused(-1, "L must", L=n)
+    for n in (0, 4097):
+        refused(-1, "B must", B=n)
+    for n in (0, 2 ** 31):
+        refused(-1, "capacity", S_cap=n, stride=2 ** 40)
+    for name in ("weight", "weight_out", "len", "budget", "idx", "new_len"):
+        refused(-1, "NULL", **{name: None})
+    refused(-1, "aligned", len=FAKE[8] + 1)
+    refused(-1, "misaligned", weight=(vp * 2)(FAKE[4], FAKE[5] + 2))
+    refused(-1, "NULL or misaligned", weight_out=(vp * 2)(FAKE[6], None))
+    refused(-1, "NULL or misaligned", idx=(vp * 2)(FAKE[9], FAKE[10] + 1))
+    refused(-1, "overlaps", weight_out=(vp * 2)(FAKE[4] + 64, FAKE[5]))
+    refused(-1, "overlaps", new_len=FAKE[8] + 8)
+    refused(-1, "weight_stride", stride=127)
+    refused(-1, "budget", budget=(i32 * 2)(64, 0))
+    refused(-1, "budget", budget=(i32 * 2)(129, 64))
+    refused(-1, "more than budget", first=60)
+    refused(-1, "more than budget", first=2 ** 31 - 1, last=2 ** 31 - 1)
+    refused(-1, "negative", last=-1)
+    refused(-1, "dtype", dtype=5)
+    refused(-1, "multiple of 16", dh=4)
+    refused(-1, "layer 1", k=(vp * 2)(FAKE[0], None))
+    refused(-1, "layer 0", v=(vp * 2)(FAKE[2] + 8, FAKE[3]))
+
+    def paged(code, text, **kw):
+        a = evict_args(**kw)
+        args = [a[n] for n in ("k", "v", "L", "B", "Hkv")] + [kw.get("pages", 40), kw.get("page", 16), a["dh"], a["dtype"], kw.get("table", FAKE[13]), kw.get("pps", 8)]
+        args += [a[n] for n in ("weight", "weight_out", "stride", "len", "budget", "first", "last", "idx", "new_len", "ws", "bytes", "stream")]
+        assert B.lib().metok_kv_evict_paged(*args) == code and text in B.metok_last_error(), (kw, B.metok_last_error())
+
+    paged(-3, "workspace")
+    paged(-1, "page_table", table=None)
+    paged(-1, "positive", page=0)
+    paged(-1, "positive", pps=0)
+    paged(-1, "positive", pages=0)
+    paged(-1, "capacity", page=2 ** 20, pps=2 ** 20)
+
+
+def test_eviction_workspace(B):
+    f = B.metok_kv_evict_workspace_bytes
+    assert f(28, 8, 4, 36992, 128, B.BF16) == B.metok_kv_compact_workspace_bytes(28, 8, 4, 36992, 128, B.BF16) > 0
+    assert f(28, 4097, 4, 128, 128, B.BF16) == 0 and f(28, 8, 4, 36992, 12, B.BF16) == 0
+
+
+def test_the_oracles_eviction_by_hand():
+    from oracle import decode_oracle as D
+    w = [5.0, 1.0, 3.0, 3.0, 0.0, 3.0, 2.0, 9.0]
+    assert D.evict(w, 8, 8, 0, 0) == list(range(8))
+    assert D.evict(w, 8, 4, 0, 0) == [0, 2, 3, 7]                # of the three 3s the first two
+    assert D.evict(w, 8, 4, 2, 1) == [0, 1, 2, 7]
+    assert D.evict(w, 8, 3, 1, 2) == [0, 6, 7]
+    assert D.evict(w, 3, 4, 0, 0) == [0, 1, 2]
+    assert D.index_list([0, 1], 4).tolist() == [0, 1, 2, 3]
+
+
+def test_the_oracles_attention_by_hand():
+    import numpy as np
+    from oracle import decode_oracle as D
+    out, lse, p = D.attend([1.0, 0.0], [[0.0, 5.0], [np.log(3.0), 1.0]], [[1.0, 0.0], [0.0, 1.0]], 1.0)
+    np.testing.assert_allclose(p, [0.25, 0.75])
+    np.testing.assert_allclose(out, [0.25, 0.75])
+    assert abs(lse - np.log(4.0)) < 1e-12
+    _, lse, p = D.attend([1.0, 0.0], [[1e9, 0.0], [-1e9, 0.0]], [[1.0, 0.0], [0.0, 1.0]], 1.0, cap=2.0)
+    np.testing.assert_allclose(p, [1 / (1 + np.exp(-4.0)), 1 / (1 + np.exp(4.0))])
+    out, lse, p = D.attend([1.0, 0.0], np.zeros((0, 2)), np.zeros((0, 2)), 1.0)
+    assert not out.any() and lse == -np.inf
+    q = np.random.default_rng(0).standard_normal((1, 4, 8))
+    k = np.random.default_rng(1).standard_normal((200, 2, 8))
+    out, lse, mean = D.decode_attention(q, [k], [k], 0.3)
+    t = torch.from_numpy(np.repeat(k.transpose(1, 0, 2), 2, axis=0))[None]
+    want = torch.nn.functional.scaled_dot_product_attention(torch.from_numpy(q)[:, :, None], t, t, scale=0.3)[:, :, 0]
+    np.testing.assert_allclose(out, want.numpy(), rtol=1e-12, atol=1e-14)
+    assert abs(mean[0].sum() - 1) < 1e-12
