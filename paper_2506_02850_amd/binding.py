@@ -228,6 +228,14 @@ def _stream() -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
+def _stream_on(index: int) -> Optional[int]:
+    """The current stream of a device that has to be the current one; None if it is not."""
+    here = torch.cuda.current_device()
+    if here != index:
+        return None
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(here)
+
+
 def _workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
 
@@ -801,6 +809,9 @@ def metok_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torc
     k_new / v_new [B, Hkv, dh]: the token's own row, stored at row lens[b] and attended to (lens is not changed).  weight [B, >= S_cap]
     float32 grows by every row's attention weight, averaged over the query heads.  scale defaults to dh ** -0.5.  Returns out [B, Hq, dh]
     and lse [B, Hq]; `out` may carry preallocated tensors under these names."""
+    res = _host.decode_attention(q, k_cache, v_cache, None, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, _stream_on)
+    if res is not None:
+        return _native(res)
     return _decode_attention(q, k_cache, v_cache, None, lens, k_new, v_new, scale, logit_cap, weight, workspace, out)
 
 
@@ -811,6 +822,9 @@ def metok_decode_attention_paged(q: torch.Tensor, k_pool: torch.Tensor, v_pool: 
     """metok_decode_attention over one layer's pools [n_pages, Hkv, page_size, dh] through page_table [B, pages_per_seq]."""
     if page_table is None:
         raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    res = _host.decode_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, _stream_on)
+    if res is not None:
+        return _native(res)
     return _decode_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out)
 
 
@@ -873,6 +887,9 @@ class _Eviction:
 
 
 def _kv_evict(k_layers, v_layers, page_table, weight, lens, budget, n_first, n_last, weight_out, idx, new_len, workspace):
+    res = _host.kv_evict(weight, lens, budget, n_first, n_last, weight_out, idx, new_len, k_layers, v_layers, page_table, workspace, _stream_on)
+    if res is not None:
+        return _native(res)
     e = _Eviction(weight, lens, budget, weight_out, idx, new_len)
     if len(k_layers) != e.L or len(v_layers) != e.L:
         raise ValueError("K buffers, V buffers and weight must have one entry per layer")
@@ -932,6 +949,9 @@ def metok_kv_evict_select(weight: Sequence[Optional[torch.Tensor]], lens: torch.
                           new_len: Optional[torch.Tensor] = None) -> Dict[str, object]:
     """The selection of metok_kv_evict alone, for caches of capacity S_cap whose rows the caller moves, or whose pages it relinks
     (metok_kv_relink_paged with these index lists)."""
+    res = _host.kv_evict_select(weight, lens, budget, n_first, n_last, weight_out, idx, new_len, S_cap, _stream_on)
+    if res is not None:
+        return _native(res)
     e = _Eviction(weight, lens, budget, weight_out, idx, new_len)
     _check(_lib.metok_kv_evict_select(*e.weights, e.L, e.B, int(S_cap), *e.lengths, int(n_first), int(n_last), *e.outputs, _stream()))
     return e.result()

@@ -35,6 +35,7 @@ struct DecodeArgs {
     int B, Hq, Hkv, group, row_blocks, rows;
     int S_cap;                   // capacity
     int page_size, pages_per_seq, n_pages;
+    uint32_t page_mul, page_shift;       // j / page_size = j * page_mul >> page_shift for 0 <= j < 2^31
     float scale;                 // without cap: of the logits in the log2 domain; with cap: scale / cap
     float cap;                   // cap in the log2 domain, 0: none
     int join_blocks, weight_blocks;      // of decode_join_kernel
@@ -88,13 +89,41 @@ __device__ __forceinline__ VideoShare find_share(const DecodeArgs& a, int want) 
     return {-1, 0, 0, 0, 0};
 }
 
+// Largest of the four lanes r, r + 16, r + 32, r + 48; each receives it.
+__device__ __forceinline__ float rows_max(float v) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+
+// tanh to about 2 units of the last place: the odd series where 1 - exp would cancel (its first missing term is 9e-9 of the result
+// at 0.25).
+__device__ __forceinline__ float tanh_of(float x) {
+    const float y = fabsf(x), x2 = x * x;
+    const float e = exp2_of(y * -2.8853900817779268f);               // exp(-2 |x|)
+    const float far = copysignf((1.f - e) * __builtin_amdgcn_rcpf(1.f + e), x);
+    const float near = x * fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, 0.021869488536155203f, -0.053968253968253968f), 0.13333333333333333f), -0.33333333333333333f), 1.f);
+    return y < 0.25f ? near : far;
+}
+
+// Read by scalar loads: written by nobody during the kernel.
+typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
+
+#ifndef NTL
+#define NTL 0
+#endif
+__device__ __forceinline__ u32x4_t load_piece(const char* p) {
+    if (NTL) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+    return *reinterpret_cast<const u32x4_t*>(p);
+}
 template <int WORDS> __device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const char* p) {
     if constexpr (WORDS == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
     else if constexpr (WORDS == 2) { const uint2 x = *reinterpret_cast<const uint2*>(p); w[0] = x.x; w[1] = x.y; }
     else {
 #pragma unroll
         for (int i = 0; i < WORDS; i += 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p + 4 * i);
+            const u32x4_t x = load_piece(p + 4 * i);
             w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
         }
     }
@@ -159,162 +188,225 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
         }
     }
 
-    // The table entry of row j, and from it the row of the pool.
-    auto page_of = [&](int j) { return table[max(0, min(j, n_cache - 1)) / a.page_size]; };
-    auto row_of = [&](int j, int page) {
-        if (j >= n_cache) return fresh && j == n_cache ? kNewRow : kNoRow;
-        if (!PAGED) return j;
-        if (page < 0 || page >= a.n_pages) return kNoRow;
-        return (page * a.Hkv + kvh) * a.page_size + j % a.page_size;
-    };
-    // rows of tile t: of the lane's K pieces and of its V parts
-    int k_row[NT], v_row[NV];
-    auto rows_of_tile = [&](int t, int page) {
-        const int j0 = t * TILE;
-        if (PAGED) {
-            const int mine = row_of(j0 + (lane & (TILE - 1)), page);
-#pragma unroll
-            for (int x = 0; x < NT; ++x) k_row[x] = __shfl(mine, 16 * x + r, 64);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) v_row[i] = __shfl(mine, 16 * (i >> 2) + 4 * c + (i & 3), 64);
-        } else {
-#pragma unroll
-            for (int x = 0; x < NT; ++x) k_row[x] = row_of(j0 + 16 * x + r, 0);
-#pragma unroll
-            for (int i = 0; i < NV; ++i) v_row[i] = row_of(j0 + 16 * (i >> 2) + 4 * c + (i & 3), 0);
-        }
-    };
+    const bool by_blocks = !PAGED || a.page_size % 16 == 0;
+    const int last = max(n_cache - 1, 0);
+    auto page_index = [&](int j) { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(j)) * a.page_mul) >> a.page_shift); };
+
     u32x4_t kf[NT][KS];
     uint32_t vf[NV][VW];
-    auto load_k = [&] {
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const char* p = row_address(k_base, k_fresh, k_row[x], RB) + c * 16;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kf[x][s] = *reinterpret_cast<const u32x4_t*>(p + s * 64);
-        }
-    };
-    auto load_v = [&] {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) load_words<VW>(vf[i], row_address(v_base, v_fresh, v_row[i], RB) + r * VW * 4);
-    };
-    auto row_mask = [&] {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) m |= (v_row[i] != kNoRow ? 1u : 0u) << i;
-        return m;
-    };
-
     f32x4_t acc[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
-    float* logits = WEIGHTS ? a.logits + (static_cast<int64_t>(b) * a.Hq + head0 + min(r, heads - 1)) * a.logit_stride : nullptr;
+    float* logits = WEIGHTS ? a.logits + (static_cast<int64_t>(b) * a.Hq + head0 + min(r, heads - 1)) * a.logit_stride + 4 * c : nullptr;
 
-    int t = t0 + wave;
-    if (t < t1) {
-        int page = PAGED ? page_of(t * TILE + (lane & (TILE - 1))) : 0;
-        rows_of_tile(t, page);
-        load_k();
-        load_v();
-        if (PAGED) page = page_of((t + kAttendWaves) * TILE + (lane & (TILE - 1)));
-        for (;;) {
-            f32x4_t s[NT];
+    struct Scores { f32x4_t x[NT]; };
+    auto scores = [&] {
+        Scores s;
 #pragma unroll
-            for (int x = 0; x < NT; ++x) {
-                s[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < NT; ++x) {
+            s.x[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int p = 0; p < KS; ++p) {
-                    if constexpr (BF16) {
-                        s[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[x][p]), __builtin_bit_cast(bf16x8_t, qf[p]), s[x], 0, 0, 0);
-                    } else {
+            for (int p = 0; p < KS; ++p) {
+                if constexpr (BF16) {
+                    s.x[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[x][p]), __builtin_bit_cast(bf16x8_t, qf[p]), s.x[x], 0, 0, 0);
+                } else {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[x][p][i]), __uint_as_float(qf[p][i]), s[x], 0, 0, 0);
-                    }
+                    for (int i = 0; i < 4; ++i) s.x[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[x][p][i]), __uint_as_float(qf[p][i]), s.x[x], 0, 0, 0);
                 }
             }
-            const uint32_t mask = row_mask();
-            const int next = t + kAttendWaves;
-            const bool more = next < t1;
-            if (more) {
-                rows_of_tile(next, page);
-                load_k();
-                if (PAGED) page = page_of((next + kAttendWaves) * TILE + (lane & (TILE - 1)));
-            }
-            if (a.cap > 0.f) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) s[i >> 2][i & 3] = a.cap * tanhf(s[i >> 2][i & 3] * a.scale);
-            } else {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) s[i >> 2][i & 3] *= a.scale;
-            }
-            if (!__all(mask == (1u << NV) - 1)) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (!((mask >> i) & 1u)) {
-                        s[i >> 2][i & 3] = -INFINITY;
-#pragma unroll
-                        for (int w = 0; w < VW; ++w) vf[i][w] = 0u;      // nothing times whatever is there must be nothing
-                    }
-            }
-            if (WEIGHTS && r < heads) {
-#pragma unroll
-                for (int x = 0; x < NT; ++x) *reinterpret_cast<f32x4_t*>(logits + t * TILE + 16 * x + 4 * c) = s[x];
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int i = 1; i < NV; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            if (__any(top > m)) {
-                const float to = fmaxf(m, top), f = exp2_of(m - (to == -INFINITY ? 0.f : to));
-                m = to;
-                l *= f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] *= f;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
-            float p[NV];
-#pragma unroll
-            for (int i = 0; i < NV; ++i) { p[i] = exp2_of(s[i >> 2][i & 3] - ref); l += p[i]; }
-            if constexpr (BF16) {
-                // a probability is the sum of two bf16 numbers, 16 of its bits: with one, the result would be as far from the exact one
-                // as its own rounding is once more; the second product hides in the wait for memory
-                typedef short operand_t __attribute__((ext_vector_type(4)));
-                uint32_t hi[NV / 2], lo[NV / 2];
-#pragma unroll
-                for (int i = 0; i < NV / 2; ++i) {
-                    hi[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
-                    lo[i] = pack_bf16x2(p[2 * i] - bf16_lo(hi[i]), p[2 * i + 1] - bf16_hi(hi[i]));
-                }
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    uint32_t f[NV / 2];
-#pragma unroll
-                    for (int i = 0; i < NV / 2; ++i) f[i] = __builtin_amdgcn_perm(vf[2 * i + 1][e >> 1], vf[2 * i][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
-                    if constexpr (NT == 2) {
-                        const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4_t{f[0], f[1], f[2], f[3]});
-                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]}), acc[e], 0, 0, 0);
-                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]}), acc[e], 0, 0, 0);
-                    } else {
-                        const operand_t v4 = __builtin_bit_cast(operand_t, make_uint2(f[0], f[1]));
-                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v4, __builtin_bit_cast(operand_t, make_uint2(hi[0], hi[1])), acc[e], 0, 0, 0);
-                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v4, __builtin_bit_cast(operand_t, make_uint2(lo[0], lo[1])), acc[e], 0, 0, 0);
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][e]), p[i], acc[e], 0, 0, 0);
-            }
-            if (!more) break;
-            load_v();
-            t = next;
         }
+        return s;
+    };
+    // Takes in the rows of tile t, those whose bit is set in `mask`.  (all: every bit is, in every lane)
+    auto take = [&](int t, Scores& s, bool all, uint32_t mask) {
+        if (a.cap > 0.f) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s.x[i >> 2][i & 3] = a.cap * tanh_of(s.x[i >> 2][i & 3] * a.scale);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s.x[i >> 2][i & 3] *= a.scale;
+        }
+        if (!all) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (!((mask >> i) & 1u)) {
+                    s.x[i >> 2][i & 3] = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < VW; ++w) vf[i][w] = 0u;      // nothing times whatever is there must be nothing
+                }
+        }
+        if (WEIGHTS && r < heads) {
+#pragma unroll
+            for (int x = 0; x < NT; ++x) *reinterpret_cast<f32x4_t*>(logits + t * TILE + 16 * x) = s.x[x];
+        }
+        float top = s.x[0][0];
+#pragma unroll
+        for (int i = 1; i < NV; ++i) top = fmaxf(top, s.x[i >> 2][i & 3]);
+        top = rows_max(top);
+        if (__any(top > m)) {
+            const float to = fmaxf(m, top), f = exp2_of(m - (to == -INFINITY ? 0.f : to));
+            m = to;
+            l *= f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] *= f;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float p[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) { p[i] = exp2_of(s.x[i >> 2][i & 3] - ref); l += p[i]; }
+        if constexpr (BF16) {
+            // a probability is the sum of two bf16 numbers, 16 of its bits: with one, the result would be as far from the exact one
+            // as its own rounding is once more; the second product hides in the wait for memory
+            typedef short operand_t __attribute__((ext_vector_type(4)));
+            uint32_t hi[NV / 2], lo[NV / 2];
+#pragma unroll
+            for (int i = 0; i < NV / 2; ++i) {
+                hi[i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+                lo[i] = pack_bf16x2(p[2 * i] - bf16_lo(hi[i]), p[2 * i + 1] - bf16_hi(hi[i]));
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                uint32_t f[NV / 2];
+#pragma unroll
+                for (int i = 0; i < NV / 2; ++i) f[i] = __builtin_amdgcn_perm(vf[2 * i + 1][e >> 1], vf[2 * i][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+                if constexpr (NT == 2) {
+                    const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4_t{f[0], f[1], f[2], f[3]});
+                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]}), acc[e], 0, 0, 0);
+                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]}), acc[e], 0, 0, 0);
+                } else {
+                    const operand_t v4 = __builtin_bit_cast(operand_t, make_uint2(f[0], f[1]));
+                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v4, __builtin_bit_cast(operand_t, make_uint2(hi[0], hi[1])), acc[e], 0, 0, 0);
+                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v4, __builtin_bit_cast(operand_t, make_uint2(lo[0], lo[1])), acc[e], 0, 0, 0);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][e]), p[i], acc[e], 0, 0, 0);
+        }
+    };
+
+    // Tiles in which every row of the cache is there are loaded by blocks of 16 neighbouring rows: one address for the wave, from scalar
+    // loads of the table, and constant offsets per lane.  A page that is none counts as row 0, and its rows are masked.
+    struct Blocks {
+        int row[NT];
+        bool ok;
+        uint32_t mask;
+    };
+    typedef int Pages __attribute__((ext_vector_type(2)));
+    const scalar_ints table_s = reinterpret_cast<scalar_ints>(reinterpret_cast<uintptr_t>(table));
+    auto pages_of = [&](int t) {
+        Pages p = {0, 0};
+        if constexpr (PAGED) {
+            p.x = table_s[page_index(min(t * TILE, last))];
+            if (NT == 2) p.y = table_s[page_index(min(t * TILE + 16, last))];
+        }
+        return p;
+    };
+    auto blocks_of = [&](int t, Pages p) {
+        Blocks f{};
+        f.ok = true;
+        f.mask = (1u << NV) - 1;
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const int j = t * TILE + 16 * x;
+            f.row[x] = j;
+            if constexpr (PAGED) {
+                const int page = x ? p.y : p.x;
+                const bool ok = page >= 0 && page < a.n_pages;
+                f.row[x] = ok ? (page * a.Hkv + kvh) * a.page_size + (j - page_index(j) * a.page_size) : 0;
+                f.ok = f.ok && ok;
+                if (!ok) f.mask &= ~(0xfu << (4 * x));
+            }
+        }
+        return f;
+    };
+    const uint32_t k_lane = r * RB + c * 16, v_lane = 4 * c * RB + r * VW * 4;
+    auto load_k_blocks = [&](const Blocks& f) {
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const char* block = k_base + static_cast<uint64_t>(static_cast<uint32_t>(f.row[x])) * RB;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[x][s] = load_piece(block + s * 64 + k_lane);
+        }
+    };
+    auto load_v_blocks = [&](const Blocks& f) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const char* block = v_base + static_cast<uint64_t>(static_cast<uint32_t>(f.row[i >> 2])) * RB;
+            load_words<VW>(vf[i], block + (i & 3) * RB + v_lane);
+        }
+    };
+    // The other tiles -- the one with the last row or the new one, all of them where pages are no multiples of 16 rows -- row by row.
+    auto row_in = [&](int t) {                             // the row that lane % TILE stands for: of the slab or pool, kNoRow or kNewRow
+        const int j = t * TILE + (lane & (TILE - 1));
+        if (j >= n_cache) return fresh && j == n_cache ? kNewRow : kNoRow;
+        if constexpr (!PAGED) return j;
+        const int index = page_index(j), page = table[index];
+        return page >= 0 && page < a.n_pages ? (page * a.Hkv + kvh) * a.page_size + (j - index * a.page_size) : kNoRow;
+    };
+    auto load_k_rows = [&](int mine) {
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+            const char* row = row_address(k_base, k_fresh, __shfl(mine, 16 * x + r, 64), RB) + c * 16;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[x][s] = load_piece(row + s * 64);
+        }
+    };
+    auto load_v_rows = [&](int mine) {
+        uint32_t mask = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int row = __shfl(mine, 16 * (i >> 2) + 4 * c + (i & 3), 64);
+            load_words<VW>(vf[i], row_address(v_base, v_fresh, row, RB) + r * VW * 4);
+            mask |= (row != kNoRow ? 1u : 0u) << i;
+        }
+        return mask;
+    };
+
+    // Both loops have K and V of a tile on their way at their top, ask for the next K as soon as the scores are taken and for
+    // the next V as soon as the sums are; nothing about these loads is conditional, so that the waits count them exactly (with the
+    // two kinds of tiles in one loop every product waited for all loads: 8 x 36992 rows 102 us).
+    const int t_whole = by_blocks ? min(t1, n_cache / TILE) : t0;      // tiles from here on go row by row
+    int t = t0 + wave;
+    if (t < t_whole) {
+        Blocks f = blocks_of(t, pages_of(t));
+        load_k_blocks(f);
+        load_v_blocks(f);
+        Pages pages = pages_of(t + kAttendWaves);
+        for (; t + kAttendWaves < t_whole; t += kAttendWaves) {
+            Scores s = scores();
+            const Blocks g = blocks_of(t + kAttendWaves, pages);
+            load_k_blocks(g);
+            pages = pages_of(t + 2 * kAttendWaves);
+            take(t, s, f.ok, f.mask);
+            load_v_blocks(g);
+            f = g;
+        }
+        Scores s = scores();
+        take(t, s, f.ok, f.mask);
+        t += kAttendWaves;
     }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
+    if (t < t1) {
+        int mine = row_in(t);
+        load_k_rows(mine);
+        uint32_t mask = load_v_rows(mine);
+        int mine_next = row_in(min(t + kAttendWaves, t1 - 1));
+        for (; t + kAttendWaves < t1; t += kAttendWaves) {
+            Scores s = scores();
+            mine = mine_next;
+            load_k_rows(mine);
+            mine_next = row_in(min(t + 2 * kAttendWaves, t1 - 1));
+            take(t, s, false, mask);
+            mask = load_v_rows(mine);
+        }
+        Scores s = scores();
+        take(t, s, false, mask);
+    }
+    l = swap16_add(l, l);
+    l = swap32_add(l, l);
 
     // the new row joins the cache: nobody reads that row of the cache in this call
     if (fresh && rb == 0 && split == sh.splits - 1 && n_cache < a.S_cap) {
@@ -567,6 +659,10 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
     a.weight_stride = weight_stride; a.logit_stride = plan.logit_stride;
     a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.group = Hq / Hkv; a.row_blocks = plan.row_blocks; a.rows = plan.rows;
     a.S_cap = static_cast<int>(S_cap); a.page_size = page_size; a.pages_per_seq = pages_per_seq; a.n_pages = static_cast<int>(n_pages);
+    int bits = 0;                // 2^bits >= page_size: ceil(2^(31 + bits) / page_size) is below 2^32 and off by less than 2^bits / page_size
+    while ((static_cast<int64_t>(1) << bits) < page_size) ++bits;
+    a.page_mul = static_cast<uint32_t>(((static_cast<uint64_t>(1) << (31 + bits)) + page_size - 1) / page_size);
+    a.page_shift = 31 + bits;
     constexpr double log2e = 1.4426950408889634074;
     a.scale = static_cast<float>(logit_cap > 0.0 ? scale / logit_cap : scale * log2e);
     a.cap = static_cast<float>(logit_cap * log2e);

@@ -9,7 +9,11 @@ namespace metok {
 constexpr int kAttendWaves = 4, kAttendThreads = 64 * kAttendWaves;
 constexpr int kAttendRows = 16;                // query rows of a workgroup: one MFMA's columns
 // Workgroups that share the rows of all videos, and the fewest tiles (of 32 or 16 rows) that one takes.
-constexpr int kAttendTarget = 512, kAttendMinTiles = 4;
+#ifndef TGT
+#define TGT 512
+#define MINT 4
+#endif
+constexpr int kAttendTarget = TGT, kAttendMinTiles = MINT;
 
 // Cache rows of a wave's tile: K and V of the next one are on their way in registers, 64 of them at most.
 constexpr int attend_tile(int esize, int dh) { return esize * dh <= 256 && esize == 2 ? 32 : 16; }

@@ -16,9 +16,11 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <cmath>
 #include <vector>
 
 #include "metok.h"
+#include "metok_decode.h"
 
 namespace {
 
@@ -147,6 +149,13 @@ template <typename F> PyObject* guarded(Py_ssize_t nargs, Py_ssize_t expected, F
 // binding.py's function for the current stream's handle, asked once everything else fits.
 inline void* stream_of(PyObject* f) {
     const Owned handle(PyObject_CallNoArgs(f));
+    return reinterpret_cast<void*>(integer(handle.o));
+}
+
+// binding.py's function for the stream of a device that has to be the current one, None if it is not: binding.py says so then.
+inline void* stream_on(PyObject* f, const at::Tensor& t) {
+    const Owned index(PyLong_FromLong(t.device().index()));
+    const Owned handle(PyObject_CallOneArg(f, index.o));
     return reinterpret_cast<void*>(integer(handle.o));
 }
 
@@ -462,6 +471,182 @@ PyObject* kv_relink_paged(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- decoding ----------------------------------------------------------------------------------------------------------
+// A tensor of this type, shape and place.
+inline const at::Tensor& fitting(PyObject* o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor& like) {
+    const at::Tensor& t = tensor(o);
+    need(t.scalar_type() == type && t.sizes() == shape && t.device() == like.device());
+    return t;
+}
+inline const at::Tensor& beside(const at::Tensor& t, const at::Tensor& like) { need(t.device() == like.device()); return t; }
+
+// q, k, v, page_table (None: dense), lens, k_new, v_new, scale, logit_cap, weight, workspace, out, stream
+PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&](Launch& launch) -> PyObject* {
+        const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]);
+        need(q.dim() == 3 && k.dim() == 4);
+        const auto type = q.scalar_type();
+        const int dt = dtype_code(q);
+        const int64_t B = q.size(0), Hq = q.size(1), dh = q.size(2), Hkv = k.size(1), rows = k.size(2);
+        need(B <= INT32_MAX && Hq <= INT32_MAX && dh <= INT32_MAX && Hkv <= INT32_MAX && rows < INT32_MAX);
+        need(k.scalar_type() == type && k.size(3) == dh && k.device() == q.device());
+        const at::Tensor& v = fitting(a[2], type, k.sizes(), q);
+        const bool paged = given(a[3]);
+        at::Tensor table;
+        int64_t cap = rows;
+        if (paged) {
+            table = beside(tensor(a[3]), q);
+            need(table.scalar_type() == at::kInt && table.dim() == 2 && table.size(0) == B && table.size(1) <= INT32_MAX);
+            cap = table.size(1) * rows;
+        } else {
+            need(k.size(0) == B);
+        }
+        const at::Tensor& lens = fitting(a[4], at::kInt, {B}, q);
+        need(given(a[5]) == given(a[6]));
+        void *k_new = nullptr, *v_new = nullptr;
+        if (given(a[5])) {
+            k_new = address(fitting(a[5], type, {B, Hkv, dh}, q));
+            v_new = address(fitting(a[6], type, {B, Hkv, dh}, q));
+        }
+        const double scale = given(a[7]) ? real(a[7]) : 1.0 / std::sqrt(static_cast<double>(dh)), logit_cap = real(a[8]);
+        at::Tensor weight;
+        if (given(a[9])) {
+            weight = beside(tensor(a[9]), q);
+            need(weight.scalar_type() == at::kFloat && weight.dim() == 2 && weight.size(0) == B);
+        }
+        const Outputs out(a[11], q);
+        const at::Tensor result = beside(out.get("out", {B, Hq, dh}, type), q), lse = beside(out.get("lse", {B, Hq}, at::kFloat), q);
+        const at::Tensor ws = beside(workspace_of(a[10], out, given(a[10]) ? 0 : metok_decode_attention_workspace_bytes(
+            static_cast<int>(B), static_cast<int>(Hq), static_cast<int>(Hkv), cap, static_cast<int>(dh), dt, weight.defined())), q);
+        Result r;
+        r.put("out", result); r.put("lse", lse);
+        void* stream = stream_on(a[12], q);
+        float* w = weight.defined() ? static_cast<float*>(address(weight)) : nullptr;
+        const int64_t w_stride = weight.defined() ? weight.size(1) : 0;
+        auto call = [&](auto f, auto... middle) {
+            return bound(f, address(q), static_cast<int>(B), static_cast<int>(Hq), static_cast<int>(Hkv), static_cast<int>(dh), dt, address(k), address(v), middle...,
+                         static_cast<const int32_t*>(address(lens)), k_new, v_new, scale, logit_cap, address(result), static_cast<float*>(address(lse)), w, w_stride,
+                         address(ws), static_cast<size_t>(ws.nbytes()), stream);
+        };
+        return answer(paged ? launch(call(&metok_decode_attention_paged, k.size(0), static_cast<int>(rows), static_cast<const int32_t*>(address(table)),
+                                          static_cast<int>(table.size(1))))
+                            : launch(call(&metok_decode_attention, rows)), r);
+    });
+}
+
+// What the eviction calls share: weight, lens, budget, n_first, n_last, weight_out, idx, new_len.
+struct Eviction {
+    std::vector<const float*> weight;
+    std::vector<float*> weight_out;
+    std::vector<int32_t*> idx;
+    std::vector<int32_t> budget;
+    at::Tensor first, lens, new_len;
+    int64_t B = 0, W = 0;
+    int L = 0, n_first = 0, n_last = 0;
+    Result result;
+
+    static PyObject** items(PyObject* o, Py_ssize_t n) {
+        need((PyList_CheckExact(o) || PyTuple_CheckExact(o)) && PySequence_Fast_GET_SIZE(o) == n);
+        return PySequence_Fast_ITEMS(o);
+    }
+    explicit Eviction(PyObject* const* a) {
+        need(PyList_CheckExact(a[0]) || PyTuple_CheckExact(a[0]));
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(a[0]);
+        need(n >= 1 && n <= METOK_MAX_LAYERS);
+        L = static_cast<int>(n);
+        PyObject **w = items(a[0], n), **to = given(a[5]) ? items(a[5], n) : w, **lists = given(a[6]) ? items(a[6], n) : nullptr;
+        for (int l = 0; l < L && !first.defined(); ++l)
+            if (given(w[l])) first = tensor(w[l]);
+        need(first.defined() && first.scalar_type() == at::kFloat && first.dim() == 2);
+        B = first.size(0); W = first.size(1);
+        need(B <= INT32_MAX);
+        if (PyLong_CheckExact(a[2])) budget.assign(static_cast<size_t>(L), int32(a[2]));
+        else {
+            PyObject** each = items(a[2], n);
+            for (int l = 0; l < L; ++l) budget.push_back(int32(each[l]));
+        }
+        n_first = int32(a[3]); n_last = int32(a[4]);
+        lens = fitting(a[1], at::kInt, {L, B}, first);
+        const Outputs fresh(Py_None, first);
+        Owned made(PyList_New(L)), moved(PyList_New(L));
+        auto place = [](const Owned& list, int l, PyObject* o) { PyList_SET_ITEM(list.o, l, o); };         // takes the reference
+        for (int l = 0; l < L; ++l) {
+            Py_INCREF(to[l]);
+            place(moved, l, to[l]);
+            if (!given(w[l])) {
+                weight.push_back(nullptr); weight_out.push_back(nullptr); idx.push_back(nullptr);
+                Py_INCREF(Py_None);
+                place(made, l, Py_None);
+                continue;
+            }
+            need(budget[l] >= 0);
+            weight.push_back(static_cast<const float*>(address(fitting(w[l], at::kFloat, {B, W}, first))));
+            weight_out.push_back(static_cast<float*>(address(fitting(to[l], at::kFloat, {B, W}, first))));
+            if (lists && given(lists[l])) {
+                idx.push_back(static_cast<int32_t*>(address(fitting(lists[l], at::kInt, {B, budget[l]}, first))));
+                Py_INCREF(lists[l]);
+                place(made, l, lists[l]);
+            } else {
+                const at::Tensor t = fresh.fresh({B, budget[l]}, at::kInt);
+                idx.push_back(static_cast<int32_t*>(address(t)));
+                place(made, l, Owned(THPVariable_Wrap(t)).release());
+            }
+        }
+        new_len = given(a[7]) ? fitting(a[7], at::kInt, {L, B}, first) : fresh.fresh({L, B}, at::kInt);
+        result.put("idx", made.release());
+        if (given(a[7])) { Py_INCREF(a[7]); result.put("new_len", a[7]); } else result.put("new_len", new_len);
+        result.put("weight", moved.release());
+    }
+    const int32_t* lengths() const { return static_cast<const int32_t*>(address(lens)); }
+    int32_t* lengths_out() const { return static_cast<int32_t*>(address(new_len)); }
+};
+
+// weight, lens, budget, n_first, n_last, weight_out, idx, new_len, k_layers, v_layers, page_table (None: dense), workspace, stream
+PyObject* kv_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 13, [&](Launch& launch) -> PyObject* {
+        Eviction e(a);
+        const Layers x(a[8], a[9]);
+        need(x.L == e.L);
+        for (int side = 8; side < 10; ++side)
+            for (int l = 0; l < x.L; ++l) {
+                const at::Tensor& t = THPVariable_Unpack(PySequence_Fast_ITEMS(a[side])[l]);
+                need(t.device() == e.first.device() && t.scalar_type() == x.first.scalar_type());
+            }
+        const bool paged = given(a[10]);
+        const int Hkv = static_cast<int>(x.first.size(1)), dh = static_cast<int>(x.first.size(3)), B = static_cast<int>(e.B);
+        const int64_t rows = x.first.size(2);
+        at::Tensor table;
+        if (paged) {
+            table = beside(tensor(a[10]), e.first);
+            need(table.scalar_type() == at::kInt && table.dim() == 2 && table.size(0) == e.B && table.size(1) <= INT32_MAX);
+        } else {
+            need(x.first.size(0) == e.B);
+        }
+        const int64_t cap = paged ? table.size(1) * rows : rows;
+        const Outputs out(Py_None, e.first);
+        const at::Tensor ws = beside(workspace_of(a[11], out, given(a[11]) ? 0 : metok_kv_evict_workspace_bytes(x.L, B, Hkv, cap, dh, x.dt)), e.first);
+        void* stream = stream_on(a[12], e.first);
+        auto call = [&](auto f, auto... middle) {
+            return bound(f, x.k.data(), x.v.data(), x.L, B, Hkv, middle..., e.weight.data(), e.weight_out.data(), e.W, e.lengths(), e.budget.data(), e.n_first, e.n_last,
+                         e.idx.data(), e.lengths_out(), address(ws), static_cast<size_t>(ws.nbytes()), stream);
+        };
+        return answer(paged ? launch(call(&metok_kv_evict_paged, x.first.size(0), static_cast<int>(rows), dh, x.dt, static_cast<const int32_t*>(address(table)),
+                                          static_cast<int>(table.size(1))))
+                            : launch(call(&metok_kv_evict, rows, dh, x.dt)), e.result);
+    });
+}
+
+// weight, lens, budget, n_first, n_last, weight_out, idx, new_len, S_cap, stream
+PyObject* kv_evict_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 10, [&](Launch& launch) -> PyObject* {
+        Eviction e(a);
+        const int64_t S_cap = integer(a[8]);
+        void* stream = stream_on(a[9], e.first);
+        return answer(launch(bound(&metok_kv_evict_select, e.weight.data(), e.weight_out.data(), e.W, e.L, static_cast<int>(e.B), S_cap, e.lengths(), e.budget.data(),
+                                   e.n_first, e.n_last, e.idx.data(), e.lengths_out(), stream)), e.result);
+    });
+}
+
 #define METOK_HOST_CALL(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {
     {"segment_compress", METOK_HOST_CALL(&segment_compress<false>)},
@@ -470,6 +655,9 @@ PyMethodDef methods[] = {
     {"prefill_prune_batched", METOK_HOST_CALL(&prefill_prune_batched)},
     {"kv_compact", METOK_HOST_CALL(&kv_compact)},
     {"kv_relink_paged", METOK_HOST_CALL(&kv_relink_paged)},
+    {"decode_attention", METOK_HOST_CALL(&decode_attention)},
+    {"kv_evict", METOK_HOST_CALL(&kv_evict)},
+    {"kv_evict_select", METOK_HOST_CALL(&kv_evict_select)},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
