@@ -43,7 +43,7 @@ extern "C" {
  *                every row j that was there before; that of the appended row is set, not added to.  Entries behind the last row are left as
  *                they were.  weight_stride >= the capacity.
  *   Limits: dh in {32, 64, 128, 256} for bf16, {32, 64, 128} for f32; Hq a multiple of Hkv; 1 <= B <= METOK_MAX_DECODE_BATCH;
- *   Hq <= 1024; capacity below 2^31 - 64; B * Hkv * ceil(Hq / Hkv / 16) and B * (capacity / 16 + 2) below 2^31.
+ *   Hq <= 1024; capacity below 2^31 - 64; B * Hkv * ceil(Hq / Hkv / 16) * (capacity / 16 + 4) below 2^31.
  *   out, lse and weight must not overlap anything else the call reads or writes.
  *   workspace    metok_decode_attention_workspace_bytes(), S_cap being the capacity (pages_per_seq * page_size of a paged cache) and
  *                with_weight whether `weight` is given.  Its contents on entry do not matter.

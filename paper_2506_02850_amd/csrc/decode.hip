@@ -1,10 +1,10 @@
 // Attention of one new token per video over the dense or paged KV cache that stage 3 leaves (Sec. 3.3), with the token's own row
 // appended and, if asked, the attention weight of every cached row accumulated (what metok_kv_evict ranks the rows by).
 //
-//   decode_attention_kernel  a workgroup's share of the rows of one (video, kv head, block of 16 query heads): scores, running
-//                            maximum and sum of the softmax, weighted sum of the values, in one pass over K and V
-//   decode_join_kernel       joins the shares of a (video, query head); and, with weights, turns the scores that the first kernel kept
-//                            into probabilities and adds their mean over the heads to the rows' weights
+//   decode_attention_kernel  every wave's tiles of the rows of all (video, kv head, block of 16 query heads): scores, running maximum and
+//                            sum of the softmax, weighted sum of the values, in one pass over K and V
+//   decode_join_kernel       joins the parts of a (video, query head) whose rows several waves had; and, with weights, turns the
+//                            scores that the first kernel kept into probabilities and adds their mean over the heads to the rows' weights
 //
 // What bounds it is the stream of K and V: 4 Hq dh operations a row on 2 Hkv dh elements, 7 operations a byte with seven query
 // heads to a kv head in bf16.  The query heads of a kv head are the columns of one MFMA, so a row is read once for all of them.
@@ -27,9 +27,10 @@ struct DecodeArgs {
     char* out;
     float* lse;                  // [B, Hq] or NULL
     float* weight;               // [B, weight_stride] or NULL
-    float* part_ml;              // [grid][rows][2]: maximum and sum of a share, log2 domain
-    float* part_o;               // [grid][rows][dh]
-    float* lse2;                 // [B, Hq]: log2 of the sum, where one workgroup had all rows
+    int2* pair_workers;          // [pairs]: first and last worker of a (video, kv head, row block)
+    float* part_ml;              // [slots][rows][2]: maximum and sum of a partial result, log2 domain
+    float* part_o;               // [slots][rows][dh]
+    float* lse2;                 // [B, Hq]: log2 of the sum, where one worker had all rows
     float* logits;               // [B, Hq, logit_stride], log2 domain
     int64_t weight_stride, logit_stride;
     int B, Hq, Hkv, group, row_blocks, rows;
@@ -38,7 +39,7 @@ struct DecodeArgs {
     uint32_t page_mul, page_shift;       // j / page_size = j * page_mul >> page_shift for 0 <= j < 2^31
     float scale;                 // without cap: of the logits in the log2 domain; with cap: scale / cap
     float cap;                   // cap in the log2 domain, 0: none
-    int join_blocks, weight_blocks;      // of decode_join_kernel
+    int join_blocks, join_lanes, weight_blocks, head_lanes;      // of decode_join_kernel
 };
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -49,44 +50,46 @@ __device__ __forceinline__ int rows_before(const DecodeArgs& a, int b) {
     return n < 0 ? 0 : (n > a.S_cap ? a.S_cap : n);
 }
 
-// The rows of a video and its workgroups.
-struct VideoShare { int b, n_cache, tiles, splits, first; };     // first: its first workgroup
+// Where a worker begins: video, its tiles and rows, unit of all its pairs; and how many units it has.
+struct Place { int b, n, tiles, at, left; };
 
-// Goes through the videos, 64 a step, one to a lane.  WANT_VIDEO: the share of video `want`; else of the video that has workgroup
-// `want`, b = -1 if there is none.  Uniform over the wave.
-template <int TILE, bool WANT_VIDEO>
-__device__ __forceinline__ VideoShare find_share(const DecodeArgs& a, int want) {
+// Goes through the videos, 64 a step, one to a lane.  An empty video has a tile, too, without rows.  Uniform over the wave.  left = 0: there is
+// no such worker.
+template <int TILE, typename DEAL>
+__device__ __forceinline__ Place find_place(const DecodeArgs& a, int worker) {
     const int lane = threadIdx.x & 63, fresh = a.k_new != nullptr, heads = a.Hkv * a.row_blocks;
-    int n = 0, tiles = 0;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
+    int n = 0, tiles = 0, before = 0;                      // units of a head of the videos before, within the 64
+    int total = 0;
+    auto look = [&](int b0) {
         const bool in = b0 + lane < a.B;
         n = in ? rows_before(a, b0 + lane) : 0;
-        tiles = in ? (n + fresh + TILE - 1) / TILE : 0;
-        total += __builtin_amdgcn_readlane(wave_inclusive_scan(tiles), 63);
-    }
-    const int64_t per64 = attend_tiles_per_group(total * heads);
-    const uint32_t per = per64 > 0x7fffffff ? 0x7fffffffu : static_cast<uint32_t>(per64);
-    int first = 0;
+        tiles = max(static_cast<int>(static_cast<uint32_t>(n + fresh + TILE - 1) / TILE), 1);
+        const int units = in ? tiles + kAttendPairCost : 0;
+        const int incl = wave_inclusive_scan(units);
+        before = incl - units;
+        return __builtin_amdgcn_readlane(incl, 63);
+    };
+    for (int b0 = 0; b0 < a.B; b0 += 64) total += look(b0);
+    const int64_t all = static_cast<int64_t>(total) * heads, first = DEAL::first(worker, all);
+    Place p{0, 0, 0, 0, static_cast<int>(DEAL::first(worker + 1, all) - first)};
+    if (worker >= DEAL::workers(all)) p.left = 0;
+    if (p.left <= 0) return p;
+    int base = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const bool in = b0 + lane < a.B;
-        if (a.B > 64) {
-            n = in ? rows_before(a, b0 + lane) : 0;
-            tiles = in ? (n + fresh + TILE - 1) / TILE : 0;
-        }
-        int splits = in ? static_cast<int>((static_cast<uint32_t>(tiles) + per - 1) / per) : 0;
-        if (in && splits < 1) splits = 1;
-        const int groups = splits * heads;
-        const int incl = wave_inclusive_scan(groups);
-        const unsigned long long hit = __ballot(in && (WANT_VIDEO ? b0 + lane == want : first + incl > want));
+        int sum = total;
+        if (a.B > 64) sum = look(b0);
+        const unsigned long long hit = __ballot(b0 + lane < a.B && static_cast<int64_t>(base + before + tiles + kAttendPairCost) * heads > first);
         if (hit) {
-            const int l = __ffsll(static_cast<long long>(hit)) - 1;
-            return {b0 + __builtin_amdgcn_readfirstlane(l), __builtin_amdgcn_readlane(n, l), __builtin_amdgcn_readlane(tiles, l), __builtin_amdgcn_readlane(splits, l),
-                    first + __builtin_amdgcn_readlane(incl - groups, l)};
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(hit)) - 1);
+            p.b = b0 + l;
+            p.n = __builtin_amdgcn_readlane(n, l);
+            p.tiles = __builtin_amdgcn_readlane(tiles, l);
+            p.at = static_cast<int>(first - static_cast<int64_t>(base + __builtin_amdgcn_readlane(before, l)) * heads);
+            break;
         }
-        first += __builtin_amdgcn_readlane(incl, 63);
+        base += sum;
     }
-    return {-1, 0, 0, 0, 0};
+    return p;
 }
 
 // Largest of the four lanes r, r + 16, r + 32, r + 48; each receives it.
@@ -110,22 +113,31 @@ __device__ __forceinline__ float tanh_of(float x) {
 // Read by scalar loads: written by nobody during the kernel.
 typedef const __attribute__((address_space(4))) int32_t* scalar_ints;
 
-#ifndef NTL
-#define NTL 0
-#endif
-__device__ __forceinline__ u32x4_t load_piece(const char* p) {
-    if (NTL) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
+template <bool STREAM> __device__ __forceinline__ u32x4_t load_piece(const char* p) {
+    if (STREAM) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p));
     return *reinterpret_cast<const u32x4_t*>(p);
 }
-template <int WORDS> __device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const char* p) {
+template <int WORDS, bool STREAM> __device__ __forceinline__ void load_words(uint32_t (&w)[WORDS], const char* p) {
     if constexpr (WORDS == 1) w[0] = *reinterpret_cast<const uint32_t*>(p);
     else if constexpr (WORDS == 2) { const uint2 x = *reinterpret_cast<const uint2*>(p); w[0] = x.x; w[1] = x.y; }
     else {
 #pragma unroll
         for (int i = 0; i < WORDS; i += 4) {
-            const u32x4_t x = load_piece(p + 4 * i);
+            const u32x4_t x = load_piece<STREAM>(p + 4 * i);
             w[i] = x.x; w[i + 1] = x.y; w[i + 2] = x.z; w[i + 3] = x.w;
         }
+    }
+}
+
+// A lane's part of a row of V: RUNS runs of neighbouring words, the runs of 16 lanes one behind the other.
+template <int RUNS, int WORDS, bool STREAM> __device__ __forceinline__ void load_part(uint32_t (&w)[WORDS], const char* row, uint32_t off) {
+    constexpr int N = WORDS / RUNS;
+#pragma unroll
+    for (int g = 0; g < RUNS; ++g) {
+        uint32_t x[N];
+        load_words<N, STREAM>(x, row + g * 16 * N * 4 + off);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[g * N + i] = x[i];
     }
 }
 
@@ -137,124 +149,228 @@ template <typename T, int DH> struct AttendShape {
     static constexpr int kKeys = kSub * 4;               // rows of V that a lane holds a part of
     static constexpr int kElems = DH / 16;               // elements of that part
     static constexpr int kWords = kElems * static_cast<int>(sizeof(T)) / 4;
+    // a part is one run of neighbouring elements, or of two runs half a row apart where it is longer than a 16-byte load
+    static constexpr int kRuns = kWords > 4 ? kWords / 4 : 1, kRun = kElems / kRuns;
 };
 
-// Rows of a cache as seen by a lane: >= 0 a row of the slab or pool, or one of these.
-constexpr int kNoRow = -1, kNewRow = -2;
-__device__ __forceinline__ const char* row_address(const char* base, const char* fresh, int row, int row_bytes) {
-    const char* p = base + static_cast<uint64_t>(static_cast<uint32_t>(row < 0 ? 0 : row)) * static_cast<uint32_t>(row_bytes);
-    return row == kNewRow ? fresh : p;
-}
+enum { kDense = 0, kBlocks = 1, kRows = 2 };              // the cache; pages of a multiple of 16 rows; other pages
 
 // A lane's place: r = lane % 16, c = lane / 16.  K Q^T is taken with the rows of K as rows of the product: the lane has query
 // head r of the scores of rows 4 c .. 4 c + 3 of every 16.  That is already the operand layout of the second product, V^T P^T with
 // the cache rows as contraction index, in the order 16 t + 4 c + i, so no value changes lanes between the two; a lane loads
-// kElems neighbouring elements r * kElems ... of its kKeys rows of V, whole rows of 16 lanes, and picks the rows' elements together
-// in registers.  The softmax state of a query head is one (maximum, sum) per lane, the sum over the lane's own rows only.
-template <typename T, int DH, bool PAGED, bool WEIGHTS>
+// its part of kKeys rows of V, 16 lanes whole rows, and picks the rows' elements together in registers.  The softmax
+// state of a query head is one (maximum, sum) per lane, the sum over the lane's own rows only.  No LDS, no barrier.
+//
+// Every wave is a worker of its own, with as many tiles as any other (one more or less), whatever videos and heads they belong to: equal bytes per
+// CU are what counts.  (Workgroups that shared the rows of one pair each, sized alike: with one to a CU as fast where they came
+// out equal, 131072 rows of 28 / 4 heads 46.7 us, 20 to 40 % slower where a third of the CUs had one more.)  K of the next tile is on
+// its way as soon as the scores are taken, V as soon as the sums are, across the end of a pair too; no load is conditional but
+// those of a new pair's queries and of the new row, so that the waits count the others exactly.
+template <typename T, int DH, int FORM, bool WEIGHTS, bool STREAM>
 __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(const DecodeArgs a) {
     using S = AttendShape<T, DH>;
     constexpr bool BF16 = sizeof(T) == 2;
     constexpr int TILE = S::kTile, NT = S::kSub, KS = S::kPieces, NV = S::kKeys, E = S::kElems, VW = S::kWords, RB = S::kRowBytes;
-    __shared__ float s_o[kAttendWaves][kAttendRows][DH + 4];
-    __shared__ float s_ml[kAttendWaves][kAttendRows][2];
-
-    const VideoShare sh = find_share<TILE, false>(a, blockIdx.x);
-    if (sh.b < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
-    const int b = sh.b, local = static_cast<int>(blockIdx.x) - sh.first;
-    const int hr = __builtin_amdgcn_readfirstlane(local / sh.splits), split = local - hr * sh.splits;
-    const int kvh = __builtin_amdgcn_readfirstlane(hr / a.row_blocks), rb = hr - kvh * a.row_blocks;
-    const int t0 = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<int64_t>(sh.tiles) * split / sh.splits));
-    const int t1 = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<int64_t>(sh.tiles) * (split + 1) / sh.splits));
+    // neighbouring workers on different CUs, so that few tiles are spread over all of them
+    const int worker = wave * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+    const Place place = find_place<TILE, Deal<attend_groups(sizeof(T), DH)>>(a, worker);
+    if (place.left <= 0) return;
     const bool fresh = a.k_new != nullptr;
-    const int n_cache = sh.n_cache;
-    const int64_t slab = static_cast<int64_t>(b) * a.Hkv + kvh;
-    const char* k_base = PAGED ? a.k : a.k + slab * a.S_cap * RB;
-    const char* v_base = PAGED ? a.v : a.v + slab * a.S_cap * RB;
-    const char* k_fresh = fresh ? a.k_new + slab * RB : nullptr;
-    const char* v_fresh = fresh ? a.v_new + slab * RB : nullptr;
-    const int32_t* table = PAGED ? a.table + static_cast<int64_t>(b) * a.pages_per_seq : nullptr;
-    const int head0 = kvh * a.group + rb * kAttendRows, heads = min(a.group - rb * kAttendRows, kAttendRows);
+    const scalar_ints lens = reinterpret_cast<scalar_ints>(reinterpret_cast<uintptr_t>(a.len));
 
-    // the query heads as the second operand of K Q^T, columns beyond them zero
-    u32x4_t qf[KS];
-    {
-        const char* p = a.q + (static_cast<int64_t>(b) * a.Hq + head0 + min(r, heads - 1)) * RB + c * 16;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            qf[s] = *reinterpret_cast<const u32x4_t*>(p + s * 64);
-            if (r >= heads) qf[s] = u32x4_t{0, 0, 0, 0};
-        }
-    }
-
-    const bool by_blocks = !PAGED || a.page_size % 16 == 0;
-    const int last = max(n_cache - 1, 0);
-    auto page_index = [&](int j) { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(j)) * a.page_mul) >> a.page_shift); };
-
-    u32x4_t kf[NT][KS];
-    uint32_t vf[NV][VW];
-    f32x4_t acc[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;
-    float* logits = WEIGHTS ? a.logits + (static_cast<int64_t>(b) * a.Hq + head0 + min(r, heads - 1)) * a.logit_stride + 4 * c : nullptr;
-
-    struct Scores { f32x4_t x[NT]; };
-    auto scores = [&] {
-        Scores s;
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            s.x[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int p = 0; p < KS; ++p) {
-                if constexpr (BF16) {
-                    s.x[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[x][p]), __builtin_bit_cast(bf16x8_t, qf[p]), s.x[x], 0, 0, 0);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s.x[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[x][p][i]), __uint_as_float(qf[p][i]), s.x[x], 0, 0, 0);
+    // A tile of a pair, its kv head and block of query heads: uniform over the wave.
+    struct Cursor { int b, kvh, rb, t, tiles, n; };
+    Cursor at;
+    at.b = __builtin_amdgcn_readfirstlane(place.b);
+    at.tiles = __builtin_amdgcn_readfirstlane(place.tiles);
+    at.n = __builtin_amdgcn_readfirstlane(place.n);
+    const int units = at.tiles + kAttendPairCost;
+    const int hr = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(place.at) / static_cast<uint32_t>(units)));
+    at.kvh = a.row_blocks == 1 ? hr : __builtin_amdgcn_readfirstlane(hr / a.row_blocks);
+    at.rb = hr - at.kvh * a.row_blocks;
+    at.t = __builtin_amdgcn_readfirstlane(place.at) - hr * units;
+    int left = __builtin_amdgcn_readfirstlane(place.left);
+    int n_ahead = lens[min(at.b + 1, a.B - 1)];
+    auto advance = [&](Cursor x) {
+        if (++x.t == x.tiles) {
+            x.t = 0;
+            if (++x.rb == a.row_blocks) {
+                x.rb = 0;
+                if (++x.kvh == a.Hkv) {
+                    x.kvh = 0;
+                    ++x.b;
+                    x.n = min(max(n_ahead, 0), a.S_cap);
+                    x.tiles = max(static_cast<int>(static_cast<uint32_t>(x.n + static_cast<int>(fresh) + TILE - 1) / TILE), 1);
+                    n_ahead = lens[min(x.b + 1, a.B - 1)];
                 }
             }
         }
-        return s;
+        return x;
     };
-    // Takes in the rows of tile t, those whose bit is set in `mask`.  (all: every bit is, in every lane)
-    auto take = [&](int t, Scores& s, bool all, uint32_t mask) {
-        if (a.cap > 0.f) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) s.x[i >> 2][i & 3] = a.cap * tanh_of(s.x[i >> 2][i & 3] * a.scale);
+    auto first_head = [&](const Cursor& x) { return x.kvh * a.group + x.rb * kAttendRows; };
+    auto n_heads = [&](const Cursor& x) { return min(a.group - x.rb * kAttendRows, kAttendRows); };
+
+    // ---- loads ----
+    auto page_index = [&](int j) { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(j)) * a.page_mul) >> a.page_shift); };
+    typedef int Pages __attribute__((ext_vector_type(2)));         // table entries of a tile's blocks, or .x of the lane's row
+    auto pages_of = [&](const Cursor& x) {
+        Pages p = {0, 0};
+        const int j0 = x.t * TILE, last = max(x.n - 1, 0);
+        if constexpr (FORM == kBlocks) {
+            const scalar_ints table = reinterpret_cast<scalar_ints>(reinterpret_cast<uintptr_t>(a.table + static_cast<int64_t>(x.b) * a.pages_per_seq));
+            p.x = table[page_index(min(j0, last))];
+            if (NT == 2) p.y = table[page_index(min(j0 + 16, last))];
+        }
+        if constexpr (FORM == kRows) p.x = a.table[static_cast<int64_t>(x.b) * a.pages_per_seq + page_index(min(j0 + (lane & (TILE - 1)), last))];
+        return p;
+    };
+    // Where a tile's rows are: by blocks of 16, the first row of each in the slab or pool and how many of it count (rows behind them are loaded as
+    // the last one), or the lane's own row; and which rows are there.
+    struct Rows { int first[NT], own; bool here, all; uint32_t pages_ok; };        // here: the tile ends before the last row; all: its pages are ones, too
+    auto rows_of = [&](const Cursor& x, Pages p) {
+        Rows f{};
+        const int j0 = x.t * TILE, last = max(x.n - 1, 0), kvh = x.kvh;
+        f.here = f.all = j0 + TILE <= x.n;
+        f.pages_ok = (1u << NT) - 1;
+        if constexpr (FORM == kRows) {
+            const int j = min(j0 + (lane & (TILE - 1)), last);
+            const bool ok = j0 + (lane & (TILE - 1)) < x.n && p.x >= 0 && p.x < a.n_pages;
+            f.own = ok ? (p.x * a.Hkv + kvh) * a.page_size + (j - page_index(j) * a.page_size) : -1;
+            f.all = f.all && __all(ok);
         } else {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) s.x[i >> 2][i & 3] *= a.scale;
-        }
-        if (!all) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (!((mask >> i) & 1u)) {
-                    s.x[i >> 2][i & 3] = -INFINITY;
-#pragma unroll
-                    for (int w = 0; w < VW; ++w) vf[i][w] = 0u;      // nothing times whatever is there must be nothing
+            for (int b = 0; b < NT; ++b) {
+                const int j = min(j0 + 16 * b, last);
+                f.first[b] = j;
+                if constexpr (FORM == kBlocks) {
+                    const int page = b ? p.y : p.x;
+                    const bool ok = page >= 0 && page < a.n_pages;
+                    f.first[b] = ok ? (page * a.Hkv + kvh) * a.page_size + (j - page_index(j) * a.page_size) : 0;
+                    if (!ok) { f.pages_ok &= ~(1u << b); f.all = false; }
                 }
+            }
         }
-        if (WEIGHTS && r < heads) {
+        return f;
+    };
+    auto slab_of = [&](const Cursor& x) { return (static_cast<int64_t>(x.b) * a.Hkv + x.kvh); };
+    auto base_of = [&](const Cursor& x, const char* cache) { return FORM == kDense ? cache + slab_of(x) * a.S_cap * RB : cache; };
+    // a row of tile x as a lane finds it: the new one, where it is that
+    auto lane_row = [&](const Cursor& x, int row, const char* cached, const char* news) {
+        return fresh && x.t * TILE + row == x.n ? news + slab_of(x) * RB : cached;
+    };
+    u32x4_t kf[NT][KS];
+    uint32_t vf[NV][VW];
+    auto load_k = [&](const Cursor& x, const Rows& f) {
+        const char* base = base_of(x, a.k);
 #pragma unroll
-            for (int x = 0; x < NT; ++x) *reinterpret_cast<f32x4_t*>(logits + t * TILE + 16 * x) = s.x[x];
+        for (int b = 0; b < NT; ++b) {
+            if constexpr (FORM == kRows) {
+                const char* row = lane_row(x, 16 * b + r, base + static_cast<uint64_t>(static_cast<uint32_t>(max(__shfl(f.own, 16 * b + r, 64), 0))) * RB, a.k_new) + c * 16;
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[b][s] = load_piece<STREAM>(row + s * 64);
+            } else {
+                const char* block = base + static_cast<uint64_t>(static_cast<uint32_t>(f.first[b])) * RB;
+                if (f.here) {
+                    const uint32_t off = r * RB + c * 16;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) kf[b][s] = load_piece<STREAM>(block + s * 64 + off);
+                } else {
+                    const char* row = lane_row(x, 16 * b + r, block + static_cast<uint32_t>(min(r, max(x.n - 1 - x.t * TILE - 16 * b, 0))) * RB, a.k_new) + c * 16;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) kf[b][s] = load_piece<STREAM>(row + s * 64);
+                }
+            }
         }
-        float top = s.x[0][0];
+    };
+    auto load_v = [&](const Cursor& x, const Rows& f) {
+        const char* base = base_of(x, a.v);
 #pragma unroll
-        for (int i = 1; i < NV; ++i) top = fmaxf(top, s.x[i >> 2][i & 3]);
+        for (int i = 0; i < NV; ++i) {
+            if constexpr (FORM == kRows) {
+                const int at_row = 16 * (i >> 2) + 4 * c + (i & 3);
+                const char* row = lane_row(x, at_row, base + static_cast<uint64_t>(static_cast<uint32_t>(max(__shfl(f.own, at_row, 64), 0))) * RB, a.v_new);
+                load_part<S::kRuns, VW, STREAM>(vf[i], row, r * (VW / S::kRuns * 4));
+            } else {
+                const char* block = base + static_cast<uint64_t>(static_cast<uint32_t>(f.first[i >> 2])) * RB;
+                if (f.here) load_part<S::kRuns, VW, STREAM>(vf[i], block + (i & 3) * RB, 4 * c * RB + r * (VW / S::kRuns * 4));
+                else {
+                    const int rows = max(x.n - 1 - x.t * TILE - 16 * (i >> 2), 0), row = 4 * c + (i & 3);
+                    load_part<S::kRuns, VW, STREAM>(vf[i], lane_row(x, 16 * (i >> 2) + row, block + static_cast<uint32_t>(min(row, rows)) * RB, a.v_new),
+                                                    r * (VW / S::kRuns * 4));
+                }
+            }
+        }
+    };
+    auto load_q = [&](const Cursor& x, u32x4_t (&q)[KS]) {
+        const int heads = n_heads(x);
+        const char* p = a.q + (static_cast<int64_t>(x.b) * a.Hq + first_head(x) + min(r, heads - 1)) * RB + c * 16;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const u32x4_t*>(p + s * 64);
+    };
+
+    // ---- one tile ----
+    u32x4_t qf[KS];
+    f32x4_t acc[E];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // row n of the cache is the new one where there is one, and is not read from the cache
+    auto new_row = [&](const Cursor& x) { return fresh && static_cast<int>(static_cast<uint32_t>(x.n) / TILE) == x.t; };
+    auto scores = [&](f32x4_t (&s)[NT]) {
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            s[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < KS; ++p) {
+                if constexpr (BF16) {
+                    s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[b][p]), __builtin_bit_cast(bf16x8_t, qf[p]), s[b], 0, 0, 0);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[b][p][i]), __uint_as_float(qf[p][i]), s[b], 0, 0, 0);
+                }
+            }
+        }
+    };
+    auto take = [&](const Cursor& x, const Rows& f, f32x4_t (&s)[NT]) {
+        if (a.cap > 0.f) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s[i >> 2][i & 3] = a.cap * tanh_of(s[i >> 2][i & 3] * a.scale);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s[i >> 2][i & 3] *= a.scale;
+        }
+        if (!f.all) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int row = 16 * (i >> 2) + 4 * c + (i & 3), j = x.t * TILE + row;
+                bool there = FORM == kRows ? __shfl(f.own, row, 64) >= 0 : j < x.n && ((f.pages_ok >> (i >> 2)) & 1u);
+                there = there || (fresh && j == x.n);
+                if (!there) s[i >> 2][i & 3] = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < VW; ++w) vf[i][w] = there ? vf[i][w] : 0u;       // nothing times whatever is there must be nothing
+            }
+        }
+        if (WEIGHTS && r < n_heads(x)) {
+            float* to = a.logits + (static_cast<int64_t>(x.b) * a.Hq + first_head(x) + r) * a.logit_stride + x.t * TILE + 4 * c;
+#pragma unroll
+            for (int b = 0; b < NT; ++b) *reinterpret_cast<f32x4_t*>(to + 16 * b) = s[b];
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 1; i < NV; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
         top = rows_max(top);
         if (__any(top > m)) {
-            const float to = fmaxf(m, top), f = exp2_of(m - (to == -INFINITY ? 0.f : to));
+            const float to = fmaxf(m, top), g = exp2_of(m - (to == -INFINITY ? 0.f : to));
             m = to;
-            l *= f;
+            l *= g;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] *= f;
+            for (int e = 0; e < E; ++e) acc[e] *= g;
         }
         const float ref = m == -INFINITY ? 0.f : m;
         float p[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) { p[i] = exp2_of(s.x[i >> 2][i & 3] - ref); l += p[i]; }
+        for (int i = 0; i < NV; ++i) { p[i] = exp2_of(s[i >> 2][i & 3] - ref); l += p[i]; }
         if constexpr (BF16) {
             // a probability is the sum of two bf16 numbers, 16 of its bits: with one, the result would be as far from the exact one
             // as its own rounding is once more; the second product hides in the wait for memory
@@ -267,15 +383,15 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
             }
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                uint32_t f[NV / 2];
+                uint32_t g[NV / 2];
 #pragma unroll
-                for (int i = 0; i < NV / 2; ++i) f[i] = __builtin_amdgcn_perm(vf[2 * i + 1][e >> 1], vf[2 * i][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+                for (int i = 0; i < NV / 2; ++i) g[i] = __builtin_amdgcn_perm(vf[2 * i + 1][e >> 1], vf[2 * i][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
                 if constexpr (NT == 2) {
-                    const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4_t{f[0], f[1], f[2], f[3]});
+                    const bf16x8_t v8 = __builtin_bit_cast(bf16x8_t, u32x4_t{g[0], g[1], g[2], g[3]});
                     acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8_t, u32x4_t{hi[0], hi[1], hi[2], hi[3]}), acc[e], 0, 0, 0);
                     acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8_t, u32x4_t{lo[0], lo[1], lo[2], lo[3]}), acc[e], 0, 0, 0);
                 } else {
-                    const operand_t v4 = __builtin_bit_cast(operand_t, make_uint2(f[0], f[1]));
+                    const operand_t v4 = __builtin_bit_cast(operand_t, make_uint2(g[0], g[1]));
                     acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v4, __builtin_bit_cast(operand_t, make_uint2(hi[0], hi[1])), acc[e], 0, 0, 0);
                     acc[e] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(v4, __builtin_bit_cast(operand_t, make_uint2(lo[0], lo[1])), acc[e], 0, 0, 0);
                 }
@@ -288,274 +404,217 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
         }
     };
 
-    // Tiles in which every row of the cache is there are loaded by blocks of 16 neighbouring rows: one address for the wave, from scalar
-    // loads of the table, and constant offsets per lane.  A page that is none counts as row 0, and its rows are masked.
-    struct Blocks {
-        int row[NT];
-        bool ok;
-        uint32_t mask;
-    };
-    typedef int Pages __attribute__((ext_vector_type(2)));
-    const scalar_ints table_s = reinterpret_cast<scalar_ints>(reinterpret_cast<uintptr_t>(table));
-    auto pages_of = [&](int t) {
-        Pages p = {0, 0};
-        if constexpr (PAGED) {
-            p.x = table_s[page_index(min(t * TILE, last))];
-            if (NT == 2) p.y = table_s[page_index(min(t * TILE + 16, last))];
+    // ---- the end of a pair, or of the worker's tiles: the result, or a part of it for the join ----
+    auto finish = [&](const Cursor& x, int begun) {         // begun: the first tile of the pair that the worker had
+        l = swap16_add(l, l);
+        l = swap32_add(l, l);
+        const int heads = n_heads(x);
+        const bool ends = x.t == x.tiles - 1, whole = begun == 0 && ends;
+        if (a.pair_workers && lane == 0) {
+            int* to = reinterpret_cast<int*>(a.pair_workers + slab_of(x) * a.row_blocks + x.rb);
+            if (begun == 0) to[0] = worker;
+            if (ends) to[1] = worker;
         }
-        return p;
-    };
-    auto blocks_of = [&](int t, Pages p) {
-        Blocks f{};
-        f.ok = true;
-        f.mask = (1u << NV) - 1;
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const int j = t * TILE + 16 * x;
-            f.row[x] = j;
-            if constexpr (PAGED) {
-                const int page = x ? p.y : p.x;
-                const bool ok = page >= 0 && page < a.n_pages;
-                f.row[x] = ok ? (page * a.Hkv + kvh) * a.page_size + (j - page_index(j) * a.page_size) : 0;
-                f.ok = f.ok && ok;
-                if (!ok) f.mask &= ~(0xfu << (4 * x));
-            }
-        }
-        return f;
-    };
-    const uint32_t k_lane = r * RB + c * 16, v_lane = 4 * c * RB + r * VW * 4;
-    auto load_k_blocks = [&](const Blocks& f) {
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const char* block = k_base + static_cast<uint64_t>(static_cast<uint32_t>(f.row[x])) * RB;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kf[x][s] = load_piece(block + s * 64 + k_lane);
-        }
-    };
-    auto load_v_blocks = [&](const Blocks& f) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const char* block = v_base + static_cast<uint64_t>(static_cast<uint32_t>(f.row[i >> 2])) * RB;
-            load_words<VW>(vf[i], block + (i & 3) * RB + v_lane);
-        }
-    };
-    // The other tiles -- the one with the last row or the new one, all of them where pages are no multiples of 16 rows -- row by row.
-    auto row_in = [&](int t) {                             // the row that lane % TILE stands for: of the slab or pool, kNoRow or kNewRow
-        const int j = t * TILE + (lane & (TILE - 1));
-        if (j >= n_cache) return fresh && j == n_cache ? kNewRow : kNoRow;
-        if constexpr (!PAGED) return j;
-        const int index = page_index(j), page = table[index];
-        return page >= 0 && page < a.n_pages ? (page * a.Hkv + kvh) * a.page_size + (j - index * a.page_size) : kNoRow;
-    };
-    auto load_k_rows = [&](int mine) {
-#pragma unroll
-        for (int x = 0; x < NT; ++x) {
-            const char* row = row_address(k_base, k_fresh, __shfl(mine, 16 * x + r, 64), RB) + c * 16;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kf[x][s] = load_piece(row + s * 64);
-        }
-    };
-    auto load_v_rows = [&](int mine) {
-        uint32_t mask = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int row = __shfl(mine, 16 * (i >> 2) + 4 * c + (i & 3), 64);
-            load_words<VW>(vf[i], row_address(v_base, v_fresh, row, RB) + r * VW * 4);
-            mask |= (row != kNoRow ? 1u : 0u) << i;
-        }
-        return mask;
-    };
-
-    // Both loops have K and V of a tile on their way at their top, ask for the next K as soon as the scores are taken and for
-    // the next V as soon as the sums are; nothing about these loads is conditional, so that the waits count them exactly (with the
-    // two kinds of tiles in one loop every product waited for all loads: 8 x 36992 rows 102 us).
-    const int t_whole = by_blocks ? min(t1, n_cache / TILE) : t0;      // tiles from here on go row by row
-    int t = t0 + wave;
-    if (t < t_whole) {
-        Blocks f = blocks_of(t, pages_of(t));
-        load_k_blocks(f);
-        load_v_blocks(f);
-        Pages pages = pages_of(t + kAttendWaves);
-        for (; t + kAttendWaves < t_whole; t += kAttendWaves) {
-            Scores s = scores();
-            const Blocks g = blocks_of(t + kAttendWaves, pages);
-            load_k_blocks(g);
-            pages = pages_of(t + 2 * kAttendWaves);
-            take(t, s, f.ok, f.mask);
-            load_v_blocks(g);
-            f = g;
-        }
-        Scores s = scores();
-        take(t, s, f.ok, f.mask);
-        t += kAttendWaves;
-    }
-    if (t < t1) {
-        int mine = row_in(t);
-        load_k_rows(mine);
-        uint32_t mask = load_v_rows(mine);
-        int mine_next = row_in(min(t + kAttendWaves, t1 - 1));
-        for (; t + kAttendWaves < t1; t += kAttendWaves) {
-            Scores s = scores();
-            mine = mine_next;
-            load_k_rows(mine);
-            mine_next = row_in(min(t + 2 * kAttendWaves, t1 - 1));
-            take(t, s, false, mask);
-            mask = load_v_rows(mine);
-        }
-        Scores s = scores();
-        take(t, s, false, mask);
-    }
-    l = swap16_add(l, l);
-    l = swap32_add(l, l);
-
-    // the new row joins the cache: nobody reads that row of the cache in this call
-    if (fresh && rb == 0 && split == sh.splits - 1 && n_cache < a.S_cap) {
-        const int to = PAGED ? table[n_cache / a.page_size] : 0;
-        if (!PAGED || (to >= 0 && to < a.n_pages)) {
-            const int64_t at = PAGED ? (static_cast<int64_t>(to) * a.Hkv + kvh) * a.page_size + n_cache % a.page_size : slab * a.S_cap + n_cache;
-            const bool value = threadIdx.x >= RB / 16;
-            const int piece = (value ? threadIdx.x - RB / 16 : threadIdx.x) * 16;
-            if (threadIdx.x < 2 * (RB / 16))
-                *reinterpret_cast<uint4*>((value ? a.v : a.k) + at * RB + piece) = *reinterpret_cast<const uint4*>((value ? v_fresh : k_fresh) + piece);
-        }
-    }
-    // the waves' results are joined: accumulator i of element e is dimension E (4 c + i) + e of query row r
-    if (c == 0) { s_ml[wave][r][0] = m; s_ml[wave][r][1] = l; }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < E; ++e) s_o[wave][r][E * (4 * c + i) + e] = acc[e][i];
-    __syncthreads();
-    // (No divergent branch lies inside another from here on: with one there, and the registers short, the compiler restored a
-    // value of all lanes where only some were enabled.)
-    const int row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * E;
-    auto joined = [&](int of, float& top, float (&f)[kAttendWaves]) {
-        top = -INFINITY;
-        float sum = 0.f;
-#pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) top = fmaxf(top, s_ml[w][of][0]);
-        const float ref = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) {
-            f[w] = exp2_of(s_ml[w][of][0] - ref);
-            sum = fmaf(s_ml[w][of][1], f[w], sum);
-        }
-        return sum;
-    };
-    float top, f[kAttendWaves], o[E];
-    const float sum = joined(row, top, f);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        o[e] = 0.f;
-#pragma unroll
-        for (int w = 0; w < kAttendWaves; ++w) o[e] = fmaf(s_o[w][row][d0 + e], f[w], o[e]);
-    }
-    const int64_t first = static_cast<int64_t>(b) * a.Hq + head0;
-    const bool whole = sh.splits == 1;
-    if (whole) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        char* to = a.out + (first + row) * RB + d0 * sizeof(T);
-        if (row < heads) {
-            if constexpr (BF16) {
-#pragma unroll
-                for (int e = 0; e < E; e += 2) reinterpret_cast<uint32_t*>(to)[e / 2] = pack_bf16x2(o[e] * inv, o[e + 1] * inv);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) reinterpret_cast<float*>(to)[e] = o[e] * inv;
-            }
-        }
-    } else if (row < heads) {
-        float* to = a.part_o + (static_cast<int64_t>(blockIdx.x) * a.rows + row) * DH + d0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) to[e] = o[e];
-    }
-    if (static_cast<int>(threadIdx.x) < heads) {
-        const float l_row = joined(threadIdx.x, top, f);
+        const int64_t head = static_cast<int64_t>(x.b) * a.Hq + first_head(x) + r;
+        const int64_t slot = (2 * static_cast<int64_t>(worker) + (begun == 0 ? 1 : 0)) * a.rows + r;
+        const float lse2 = l == 0.f ? -INFINITY : m + log2_of(l), inv = l == 0.f ? 0.f : 1.f / l;
+        // accumulator i of element e: element kRun (4 c + i) + e % kRun of run e / kRun
+        constexpr int N = S::kRun;
         if (whole) {
-            const float lse2 = l_row == 0.f ? -INFINITY : top + log2_of(l_row);
-            if (a.lse) a.lse[first + threadIdx.x] = lse2 * 0.693147180559945309f;
-            if (WEIGHTS) a.lse2[first + threadIdx.x] = lse2;
+            if (r < heads) {
+#pragma unroll
+                for (int g = 0; g < S::kRuns; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        char* to = a.out + head * RB + (g * 16 * N + N * (4 * c + i)) * static_cast<int>(sizeof(T));
+#pragma unroll
+                        for (int e = 0; e < N; e += BF16 ? 2 : 1) {
+                            if constexpr (BF16) reinterpret_cast<uint32_t*>(to)[e / 2] = pack_bf16x2(acc[g * N + e][i] * inv, acc[g * N + e + 1][i] * inv);
+                            else reinterpret_cast<float*>(to)[e] = acc[g * N + e][i] * inv;
+                        }
+                    }
+            }
+            if (lane < heads && a.lse) a.lse[head] = lse2 * 0.693147180559945309f;
+            if (WEIGHTS && lane < heads) a.lse2[head] = lse2;
         } else {
-            reinterpret_cast<float2*>(a.part_ml)[static_cast<int64_t>(blockIdx.x) * a.rows + threadIdx.x] = make_float2(top, l_row);
+            if (r < heads) {
+                float* to = a.part_o + slot * DH;
+#pragma unroll
+                for (int g = 0; g < S::kRuns; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) to[g * 16 * N + N * (4 * c + i) + e] = acc[g * N + e][i];
+            }
+            if (lane < heads) reinterpret_cast<float2*>(a.part_ml)[slot] = make_float2(m, l);
         }
+    };
+    // the new row joins the cache: nobody reads that row of the cache in this call
+    auto append = [&](const Cursor& x) {
+        if (!new_row(x) || x.rb != 0 || x.n >= a.S_cap) return;
+        int64_t to = slab_of(x) * a.S_cap + x.n;
+        if constexpr (FORM != kDense) {
+            const int index = page_index(x.n), page = a.table[static_cast<int64_t>(x.b) * a.pages_per_seq + index];
+            if (page < 0 || page >= a.n_pages) return;
+            to = (static_cast<int64_t>(page) * a.Hkv + x.kvh) * a.page_size + (x.n - index * a.page_size);
+        }
+        constexpr int P = RB / 16;
+        if (lane < 2 * P) {
+            const bool value = lane >= P;
+            const int piece = (value ? lane - P : lane) * 16;
+            *reinterpret_cast<uint4*>((value ? a.v : a.k) + to * RB + piece) = *reinterpret_cast<const uint4*>((value ? a.v_new : a.k_new) + slab_of(x) * RB + piece);
+        }
+    };
+
+    if (at.t >= at.tiles) {                                // behind a pair: on to the next one, if there is one
+        left -= at.tiles + kAttendPairCost - at.t;
+        if (left <= 0) return;
+        at.t = at.tiles - 1;
+        at = advance(at);
     }
+    int begun = at.t;                                      // first tile of the pair that the worker has
+    load_q(at, qf);
+    Rows rows = rows_of(at, pages_of(at));
+    load_k(at, rows);
+    load_v(at, rows);
+    u32x4_t q_next[KS];
+    for (;;) {
+        const bool ends = at.t == at.tiles - 1;
+        left -= ends ? 1 + kAttendPairCost : 1;
+        if (left <= 0) break;
+        const Cursor next = advance(at);
+        const Pages pages = pages_of(next);
+        f32x4_t s[NT];
+        scores(s);
+        const Rows rows_next = rows_of(next, pages);
+        load_k(next, rows_next);
+        if (ends) load_q(next, q_next);
+        take(at, rows, s);
+        if (ends) {
+            finish(at, begun);
+            append(at);
+            begun = 0;
+            m = -INFINITY; l = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < KS; ++p) qf[p] = q_next[p];
+        }
+        load_v(next, rows_next);
+        at = next;
+        rows = rows_next;
+    }
+    f32x4_t s[NT];
+    scores(s);
+    take(at, rows, s);
+    finish(at, begun);
+    append(at);
 }
 
 constexpr int kJoinThreads = 256;
 constexpr int kWeightRows = 256;       // cache rows a workgroup adds up at a time: four to a lane
+// Up to so many workgroups a head's elements are spread over several of them, 32 each: with few heads every one has many parts (one
+// video of 2307 rows, 28 heads: 10.1 us a call with one workgroup a head, 9.0 with four).
+constexpr int kJoinSpread = 512;
 
-// log2 of the sum of a query head's shares, +inf where no row counts; all lanes of the wave.
-__device__ __forceinline__ float wave_lse2(const DecodeArgs& a, const VideoShare& sh, int head) {
+// (m, l) stands for the sum l 2^m.
+__device__ __forceinline__ void add_sum(float& m, float& l, float m2, float l2) {
+    const float to = fmaxf(m, m2), ref = to == -INFINITY ? 0.f : to;
+    l = l * exp2_of(m - ref) + l2 * exp2_of(m2 - ref);
+    m = to;
+}
+
+// The workers of a query head's pair, and the place of their partial results.
+struct HeadParts {
+    int first, n, rows, row;
+    __device__ __forceinline__ int64_t slot(int p) const { return static_cast<int64_t>(2 * (first + p) + (p == 0)) * rows + row; }
+};
+__device__ __forceinline__ HeadParts parts_of(const DecodeArgs& a, int b, int head) {
     const int kvh = head / a.group, qi = head - kvh * a.group, rb = qi / kAttendRows;
-    float lse2;
-    if (sh.splits == 1) lse2 = a.lse2[static_cast<int64_t>(sh.b) * a.Hq + head];
-    else {
-        const int64_t slot0 = static_cast<int64_t>(sh.first + (kvh * a.row_blocks + rb) * sh.splits) * a.rows + (qi - rb * kAttendRows);
-        float m = -INFINITY, l = 0.f;
-        for (int p = threadIdx.x & 63; p < sh.splits; p += 64) {
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (slot0 + static_cast<int64_t>(p) * a.rows));
-            const float to = fmaxf(m, ml.x), ref = to == -INFINITY ? 0.f : to;
-            l = l * exp2_of(m - ref) + ml.y * exp2_of(ml.x - ref);
-            m = to;
-        }
-#pragma unroll
-        for (int off = 32; off; off >>= 1) {
-            const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), to = fmaxf(m, m2), ref = to == -INFINITY ? 0.f : to;
-            l = l * exp2_of(m - ref) + l2 * exp2_of(m2 - ref);
-            m = to;
-        }
-        lse2 = l == 0.f ? -INFINITY : m + log2_of(l);
-    }
-    return lse2 == -INFINITY ? INFINITY : lse2;
+    const int2 w = a.pair_workers[(static_cast<int64_t>(b) * a.Hkv + kvh) * a.row_blocks + rb];
+    return {w.x, w.y - w.x + 1, a.rows, qi - rb * kAttendRows};
 }
 
 template <typename T, int DH>
 __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeArgs a) {
-    constexpr int TILE = attend_tile(sizeof(T), DH);
-    constexpr int LANES = DH / 4, GROUPS = kJoinThreads / LANES;       // lanes of a row, rows at a time
-    __shared__ float s_x[1024];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
     if (static_cast<int>(blockIdx.x) < a.join_blocks) {
-        // one (video, query head)
+        // One (video, query head), or 4 join_lanes of its elements.  Every wave sums up the parts' statistics for itself; the parts of the output
+        // are on their way meanwhile, the first kAhead of every group of lanes.
+        constexpr int kAhead = 4;
         __shared__ float4 s_part[kJoinThreads];
-        const int b = blockIdx.x / a.Hq, head = blockIdx.x - b * a.Hq;
-        const VideoShare sh = find_share<TILE, true>(a, b);
-        if (sh.splits == 1) return;
-        const int kvh = head / a.group, qi = head - kvh * a.group, rb = qi / kAttendRows;
-        const int64_t slot0 = static_cast<int64_t>(sh.first + (kvh * a.row_blocks + rb) * sh.splits) * a.rows + (qi - rb * kAttendRows);
-        const float lse2 = wave_lse2(a, sh, head);                      // +inf: the factors below are 0
-        const int g = threadIdx.x / LANES, x = threadIdx.x % LANES;
+        const int lanes = a.join_lanes, groups = kJoinThreads / lanes, pieces = DH / 4 / lanes;
+        const int unit = blockIdx.x / pieces, piece = blockIdx.x - unit * pieces;
+        const int b = unit / a.Hq, head = unit - b * a.Hq;
+        const HeadParts parts = parts_of(a, b, head);
+        if (parts.n == 1) return;
+        const int g = threadIdx.x / lanes, x = threadIdx.x - g * lanes;
+        const float* part = a.part_o + (piece * lanes + x) * 4;
+        float4 ahead[kAhead];
+        float ahead_m[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t slot = parts.slot(min(g + k * groups, parts.n - 1));
+            ahead[k] = *reinterpret_cast<const float4*>(part + slot * DH);
+            ahead_m[k] = ml[slot].x;
+        }
+        float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+        for (int p = lane; p < parts.n; p += 64) {
+            const float2 v = ml[parts.slot(p)];
+            add_sum(m, l, v.x, v.y);
+        }
+#pragma unroll
+        for (int off = 32; off; off >>= 1) add_sum(m, l, __shfl_xor(m, off, 64), __shfl_xor(l, off, 64));
+        const float lse2 = l == 0.f ? INFINITY : m + log2_of(l);            // +inf, no row counts: the factors below are 0
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int p = g; p < sh.splits; p += GROUPS) {
-            const int64_t slot = slot0 + static_cast<int64_t>(p) * a.rows;
-            const float f = exp2_of(a.part_ml[2 * slot] - lse2);
-            const float4 v = *reinterpret_cast<const float4*>(a.part_o + slot * DH + x * 4);
-            o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+        auto add = [&](const float4& v, float f) { o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w); };
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (g + k * groups < parts.n) add(ahead[k], exp2_of(ahead_m[k] - lse2));
+#pragma unroll 4
+        for (int p = g + kAhead * groups; p < parts.n; p += groups) {
+            const int64_t slot = parts.slot(p);
+            add(*reinterpret_cast<const float4*>(part + slot * DH), exp2_of(ml[slot].x - lse2));
         }
         s_part[threadIdx.x] = o;
         __syncthreads();
         if (g == 0) {
-            for (int k = 1; k < GROUPS; ++k) {
-                const float4 v = s_part[k * LANES + x];
+#pragma unroll 8
+            for (int k = 1; k < groups; ++k) {
+                const float4 v = s_part[k * lanes + x];
                 o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
             }
+            const int64_t at = static_cast<int64_t>(b) * a.Hq + head, to = at * DH + (piece * lanes + x) * 4;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(a.out + to * 2) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
+            else *reinterpret_cast<float4*>(a.out + to * 4) = o;
+        }
+        if (threadIdx.x == 0 && piece == 0) {
             const int64_t at = static_cast<int64_t>(b) * a.Hq + head;
-            if constexpr (sizeof(T) == 2)
-                *reinterpret_cast<uint2*>(a.out + (at * DH + x * 4) * 2) = make_uint2(pack_bf16x2(o.x, o.y), pack_bf16x2(o.z, o.w));
-            else *reinterpret_cast<float4*>(a.out + (at * DH + x * 4) * 4) = o;
-            if (x == 0 && a.lse) a.lse[at] = lse2 == INFINITY ? -INFINITY : lse2 * 0.693147180559945309f;
+            if (a.lse) a.lse[at] = lse2 == INFINITY ? -INFINITY : lse2 * 0.693147180559945309f;
         }
         return;
     }
-    // rows of one video: every lane has four neighbouring rows, the waves share the heads
+    // Rows of one video: every lane has four neighbouring rows, the waves share the heads.
+    __shared__ float s_lse2[1024];
     __shared__ float4 s_sum[kJoinThreads];
     const int w = static_cast<int>(blockIdx.x) - a.join_blocks, b = w / a.weight_blocks, first = w - b * a.weight_blocks;
-    const VideoShare sh = find_share<TILE, true>(a, b);
-    const int fresh = a.k_new != nullptr, n = min(sh.n_cache + fresh, a.S_cap);       // rows that have a place
+    const int fresh = a.k_new != nullptr, n_cache = rows_before(a, b), n = min(n_cache + fresh, a.S_cap);       // rows that have a place
     if (static_cast<int64_t>(first) * kWeightRows >= n) return;
-    for (int h = wave; h < a.Hq; h += kJoinThreads / 64) {
-        const float v = wave_lse2(a, sh, h);
-        if (lane == 0) s_x[h] = v;
+    // log2 of the heads' sums, +inf where no row counts: a.head_lanes neighbouring lanes to a head
+    for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / a.head_lanes) {
+        const int h = min(h0 + static_cast<int>(threadIdx.x) / a.head_lanes, a.Hq - 1), part = threadIdx.x % a.head_lanes;
+        const HeadParts parts = parts_of(a, b, h);
+        float m = -INFINITY, l = 0.f;
+#pragma unroll 4
+        for (int p = part; p < (parts.n > 1 ? parts.n : 0); p += a.head_lanes) {
+            const float2 v = ml[parts.slot(p)];
+            add_sum(m, l, v.x, v.y);
+        }
+        for (int off = a.head_lanes / 2; off; off >>= 1) add_sum(m, l, __shfl_xor(m, off, 64), __shfl_xor(l, off, 64));
+        const float lse2 = parts.n == 1 ? a.lse2[static_cast<int64_t>(b) * a.Hq + h] : m + log2_of(l);
+        if (part == 0) s_lse2[h] = lse2 > -INFINITY ? lse2 : INFINITY;       // log2(0) is -inf
     }
     __syncthreads();
     const float inv = 1.f / static_cast<float>(a.Hq);
@@ -564,9 +623,10 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         if (j < n) {
             const float* p = a.logits + static_cast<int64_t>(b) * a.Hq * a.logit_stride + j;
+#pragma unroll 8
             for (int h = wave; h < a.Hq; h += kJoinThreads / 64) {
                 const float4 x = *reinterpret_cast<const float4*>(p + h * a.logit_stride);
-                const float z = s_x[h];
+                const float z = s_lse2[h];
                 sum.x += exp2_of(x.x - z); sum.y += exp2_of(x.y - z); sum.z += exp2_of(x.z - z); sum.w += exp2_of(x.w - z);
             }
         }
@@ -578,25 +638,38 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
 #pragma unroll
             for (int k = 0; k < kJoinThreads / 64; ++k) total += reinterpret_cast<const float*>(s_sum + 64 * k)[threadIdx.x];
             float* out = a.weight + static_cast<int64_t>(b) * a.weight_stride + mine;
-            *out = (mine < sh.n_cache ? *out : 0.f) + total * inv;
+            *out = (mine < n_cache ? *out : 0.f) + total * inv;
         }
         __syncthreads();
     }
 }
 
+template <typename T, int DH, int FORM, bool STREAM>
+static void launch_attention(const DecodeArgs& a, unsigned groups, hipStream_t st) {
+    if (a.weight) hipLaunchKernelGGL((decode_attention_kernel<T, DH, FORM, true, STREAM>), dim3(groups), dim3(kAttendThreads), 0, st, a);
+    else hipLaunchKernelGGL((decode_attention_kernel<T, DH, FORM, false, STREAM>), dim3(groups), dim3(kAttendThreads), 0, st, a);
+}
+
+// Caches of more than this many bytes are read with the streaming hint: 375 MB (4 x 4571 rows, 40 heads of 128) 91 us without, 81 with; 606 MB
+// 109 and 98; a tenth of them, that the memory-side cache still holds from the call before, 16.5 and 18.1 (67 MB).
+constexpr int64_t kStreamBytes = 128 << 20;
+
 template <typename T, int DH>
-static int launch_attend(const DecodeArgs& a, const AttendPlan& plan, hipStream_t st) {
-    const dim3 grid(static_cast<unsigned>(plan.grid)), block(kAttendThreads);
-    if (a.table) {
-        if (a.weight) hipLaunchKernelGGL((decode_attention_kernel<T, DH, true, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((decode_attention_kernel<T, DH, true, false>), grid, block, 0, st, a);
-    } else {
-        if (a.weight) hipLaunchKernelGGL((decode_attention_kernel<T, DH, false, true>), grid, block, 0, st, a);
-        else hipLaunchKernelGGL((decode_attention_kernel<T, DH, false, false>), grid, block, 0, st, a);
-    }
+static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) {
+    const int64_t bytes = static_cast<int64_t>(a.B) * a.Hkv * a.S_cap * DH * static_cast<int64_t>(sizeof(T)) * 2;
+    const unsigned groups = static_cast<unsigned>(plan.grid);
+    const bool stream = bytes > kStreamBytes;
+    if (!a.table) stream ? launch_attention<T, DH, kDense, true>(a, groups, st) : launch_attention<T, DH, kDense, false>(a, groups, st);
+    else if (a.page_size % 16 != 0) launch_attention<T, DH, kRows, false>(a, groups, st);
+    else stream ? launch_attention<T, DH, kBlocks, true>(a, groups, st) : launch_attention<T, DH, kBlocks, false>(a, groups, st);
     int rc = check_launch("decode attention");
     if (rc) return rc;
-    const int64_t blocks = a.join_blocks + static_cast<int64_t>(a.weight ? a.B : 0) * a.weight_blocks;
+    const int64_t units = plan.joined ? static_cast<int64_t>(a.B) * a.Hq : 0;
+    const int64_t weight_blocks = a.weight ? static_cast<int64_t>(a.B) * a.weight_blocks : 0;
+    // few heads have many parts each: their elements over several workgroups
+    a.join_lanes = units * (DH / 4 / 8) <= kJoinSpread ? 8 : DH / 4;
+    a.join_blocks = static_cast<int>(units * (DH / 4 / a.join_lanes));
+    const int64_t blocks = a.join_blocks + weight_blocks;
     if (blocks == 0) return METOK_OK;
     hipLaunchKernelGGL((decode_join_kernel<T, DH>), dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads), 0, st, a);
     return check_launch("decode join");
@@ -610,7 +683,7 @@ static const char* bad_shape(int B, int Hq, int Hkv, int64_t S_cap, int dh, int 
     if (dh != 32 && dh != 64 && dh != 128 && !(dh == 256 && dtype == METOK_BF16)) return "dh must be 32, 64, 128 or (bf16) 256";
     if (S_cap < 1 || S_cap >= INT32_MAX - 64) return "the capacity must be in [1, 2^31 - 64)";
     const int64_t pairs = static_cast<int64_t>(B) * Hkv * ((Hq / Hkv + kAttendRows - 1) / kAttendRows);
-    if (pairs + kAttendTarget > INT32_MAX || static_cast<int64_t>(B) * (S_cap / 16 + 2) > INT32_MAX) return "too many rows";
+    if (pairs * (S_cap / 16 + 4) > INT32_MAX) return "too many rows";
     return nullptr;
 }
 
@@ -654,6 +727,7 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
     a.k_new = static_cast<const char*>(k_new); a.v_new = static_cast<const char*>(v_new);
     a.len = len; a.table = table; a.out = static_cast<char*>(out); a.lse = lse; a.weight = weight;
     char* ws = static_cast<char*>(workspace);
+    a.pair_workers = plan.joined || weight ? reinterpret_cast<int2*>(ws + plan.pair_workers) : nullptr;
     a.part_ml = reinterpret_cast<float*>(ws + plan.part_ml); a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
     a.lse2 = reinterpret_cast<float*>(ws + plan.lse2); a.logits = reinterpret_cast<float*>(ws + plan.logits);
     a.weight_stride = weight_stride; a.logit_stride = plan.logit_stride;
@@ -666,10 +740,11 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
     constexpr double log2e = 1.4426950408889634074;
     a.scale = static_cast<float>(logit_cap > 0.0 ? scale / logit_cap : scale * log2e);
     a.cap = static_cast<float>(logit_cap * log2e);
-    a.join_blocks = plan.joined ? B * Hq : 0;
     // every workgroup of the weights sums up the heads' shares for itself: enough of them for the chip, not more
     const int64_t most = (S_cap + kWeightRows - 1) / kWeightRows, enough = (1024 + B - 1) / B;
     a.weight_blocks = static_cast<int>(most < enough ? most : enough);
+    a.head_lanes = 64;
+    while (a.head_lanes > 1 && Hq * a.head_lanes > kJoinThreads) a.head_lanes /= 2;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == METOK_BF16) {
         if (dh == 32) return launch_attend<bf16_t, 32>(a, plan, st);

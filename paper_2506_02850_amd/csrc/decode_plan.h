@@ -7,34 +7,43 @@
 namespace metok {
 
 constexpr int kAttendWaves = 4, kAttendThreads = 64 * kAttendWaves;
-constexpr int kAttendRows = 16;                // query rows of a workgroup: one MFMA's columns
-// Workgroups that share the rows of all videos, and the fewest tiles (of 32 or 16 rows) that one takes.
-#ifndef TGT
-#define TGT 512
-#define MINT 4
-#endif
-constexpr int kAttendTarget = TGT, kAttendMinTiles = MINT;
-
-// Cache rows of a wave's tile: K and V of the next one are on their way in registers, 64 of them at most.
+constexpr int kAttendRows = 16;                // query rows of a wave: one MFMA's columns
+// Cache rows of a tile: K and V of the next one are on their way in registers, 64 of them at most.
 constexpr int attend_tile(int esize, int dh) { return esize * dh <= 256 && esize == 2 ? 32 : 16; }
+// Workgroups of a large call: one per CU, two where a tile is only 4 KB (8 x 73980 rows of 4 heads of 32 bf16: 68 us with one, 57 with two, 57 with
+// four; of 2 heads of 64: 58, 62).
+constexpr int attend_groups(int esize, int dh) { return 2 * attend_tile(esize, dh) * esize * dh <= 4096 ? 512 : 256; }
+
+// The tiles of all (video, kv head, row block) pairs, one pair behind the other, are dealt out evenly to the waves, the workers.  The end of a
+// pair takes a worker about as long as a tile, so every pair counts kAttendPairCost tiles more than it has; they lie behind its own (32 videos of 0
+// to 8191 rows, 32 heads on 8: 41 us without, 32 with one, 31.5 with two; many short pairs fell to few workers).
+// Worker w of n has units [w T / n, (w + 1) T / n), or kAttendMinTiles of them where there are few (2307 rows of 28 heads on 4: 9.2 us with one, 9.3
+// with two, 11 with four; 2 x 5033 of 14 on 2 in fp32: 12.3, 10.7, 11.1: with one there are more parts to join).
+constexpr int kAttendMinTiles = 2, kAttendPairCost = 1;
+template <int GROUPS> struct Deal {
+    static constexpr int kWorkers = GROUPS * kAttendWaves;
+    static_assert((kWorkers & (kWorkers - 1)) == 0, "a worker's first unit is a shift away");
+    static constexpr int64_t workers(int64_t units) {
+        const int64_t few = (units + kAttendMinTiles - 1) / kAttendMinTiles;
+        return few < kWorkers ? few : kWorkers;
+    }
+    static constexpr int64_t first(int64_t worker, int64_t units) {
+        const int64_t at = units < static_cast<int64_t>(kAttendMinTiles) * kWorkers ? worker * kAttendMinTiles : worker * units / kWorkers;
+        return at < units ? at : units;
+    }
+};
 
 struct AttendPlan {
     int tile;              // cache rows of a tile
     int row_blocks;        // blocks of kAttendRows query heads of a kv head
     int rows;              // query rows of a partial result
     int64_t pairs;         // (video, kv head, row block): what is split over the rows of the cache
-    int64_t grid;          // workgroups, and slots for partial results
-    bool joined;           // false: every pair is one workgroup's, whatever the lengths
+    int64_t grid;          // workgroups
+    int64_t workers;       // at most
+    bool joined;           // false: every pair is one tile, whatever the lengths
     int64_t logit_stride;  // logits of a (video, query head), 0: not kept
-    size_t part_ml, part_o, lse2, logits, bytes;       // offsets in the workspace, and its size
+    size_t pair_workers, part_ml, part_o, lse2, logits, bytes;       // offsets in the workspace, and its size
 };
-
-// Tiles a workgroup takes at most, from the tiles of all pairs: kAttendTarget + pairs workgroups are enough for any lengths, because
-// a pair has at most one workgroup more than its share.
-constexpr int64_t attend_tiles_per_group(int64_t tiles_of_pairs) {
-    const int64_t share = (tiles_of_pairs + kAttendTarget - 1) / kAttendTarget;
-    return share > kAttendMinTiles ? share : kAttendMinTiles;
-}
 
 // `capacity` rows at most, one more with a new row.
 constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int dh, int esize, bool with_weight) {
@@ -45,10 +54,11 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     p.rows = group < kAttendRows ? group : kAttendRows;
     p.pairs = static_cast<int64_t>(B) * Hkv * p.row_blocks;
     const int64_t most = (capacity + 1 + p.tile - 1) / p.tile;                       // tiles of the longest video
-    const int64_t splits = (most + kAttendMinTiles - 1) / kAttendMinTiles;
-    p.joined = splits > 1;
-    p.grid = p.pairs + kAttendTarget;
-    if (splits <= kAttendTarget && p.pairs * splits < p.grid) p.grid = p.pairs * splits;
+    p.joined = most > 1;
+    const int groups = attend_groups(esize, dh);
+    const int64_t few = ((most + kAttendPairCost) * p.pairs + kAttendMinTiles - 1) / kAttendMinTiles;      // workers, with a workgroup each
+    p.grid = few < groups ? few : groups;
+    p.workers = static_cast<int64_t>(groups) * kAttendWaves;
     p.logit_stride = with_weight ? (capacity + 1 + 31) / 32 * 32 : 0;
     size_t at = 0;
     auto take = [&at](size_t floats) {
@@ -56,7 +66,10 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
         at += (floats * sizeof(float) + 255) / 256 * 256;
         return here;
     };
-    const size_t slots = p.joined ? static_cast<size_t>(p.grid) * p.rows : 0;
+    p.pair_workers = take(p.joined || with_weight ? static_cast<size_t>(p.pairs) * 2 : 0);
+    // a worker leaves at most two partial results: of the pair that an earlier worker began (slot 2 w) and of the one that it begins and a
+    // later one ends (slot 2 w + 1)
+    const size_t slots = p.joined ? static_cast<size_t>(2 * p.workers) * p.rows : 0;
     p.part_ml = take(slots * 2);
     p.part_o = take(slots * dh);
     p.lse2 = take(with_weight ? static_cast<size_t>(B) * Hq : 0);

@@ -80,6 +80,7 @@ def test_refused_attention_calls(B):
     for s in (0, -5, 2 ** 31 - 64, 2 ** 40):
         refused(-1, "capacity", S_cap=s, stride=2 ** 41)
     refused(-1, "too many rows", B=4096, S_cap=2 ** 30, stride=2 ** 41)
+    refused(-1, "too many rows", B=64, Hq=1024, Hkv=64, S_cap=2 ** 24, stride=2 ** 41)
     big = 1 << 40
     refused(-1, "overlaps", out=FAKE[0], bytes=big)
     refused(-1, "overlaps", lse=FAKE[6], bytes=big)
@@ -113,9 +114,9 @@ def test_refused_paged_attention_calls(B):
 
 def test_workspace_sizes(B):
     f = B.metok_decode_attention_workspace_bytes
-    assert f(1, 28, 4, 100, 128, B.BF16) == 0                           # one workgroup per kv head: nothing to join
+    assert f(1, 28, 4, 31, 128, B.BF16) == 0                            # one tile per kv head: nothing to join
     small, big = f(8, 28, 4, 36992, 128, B.BF16), f(8, 28, 4, 36992, 128, B.BF16, True)
-    assert 0 < small < 16 << 20
+    assert 0 < small < 24 << 20
     assert big - small >= 8 * 28 * 36993 * 4                            # the logits
     assert f(8, 28, 4, 36992, 128, B.F32) > 0
     for bad in ((0, 28, 4, 100, 128, 1), (1, 28, 5, 100, 128, 1), (1, 28, 4, 0, 128, 1), (1, 28, 4, 100, 48, 1), (1, 28, 4, 100, 256, 0), (1, 28, 4, 100, 128, 7)):
@@ -123,46 +124,91 @@ def test_workspace_sizes(B):
 
 
 PLAN = r"""
+#include <initializer_list>
 #include "decode_plan.h"
 using namespace metok;
 extern "C" void attend_plan(int B, int Hq, int Hkv, int64_t cap, int dh, int esize, int w, int64_t* o) {
     const AttendPlan p = plan_attend(B, Hq, Hkv, cap, dh, esize, w != 0);
-    for (int64_t v : {int64_t(p.tile), int64_t(p.row_blocks), int64_t(p.rows), p.pairs, p.grid, int64_t(p.joined), p.logit_stride, int64_t(p.part_ml),
-                      int64_t(p.part_o), int64_t(p.lse2), int64_t(p.logits), int64_t(p.bytes)}) *o++ = v;
+    for (int64_t v : {int64_t(p.tile), int64_t(p.row_blocks), int64_t(p.rows), p.pairs, p.grid, p.workers, int64_t(p.joined), p.logit_stride, int64_t(p.pair_workers),
+                      int64_t(p.part_ml), int64_t(p.part_o), int64_t(p.lse2), int64_t(p.logits), int64_t(p.bytes), int64_t(attend_groups(esize, dh))}) *o++ = v;
 }
-extern "C" int64_t tiles_per_group(int64_t t) { return attend_tiles_per_group(t); }
+extern "C" int64_t workers(int groups, int64_t units) { return groups == 512 ? Deal<512>::workers(units) : Deal<256>::workers(units); }
+extern "C" int64_t first(int groups, int64_t w, int64_t units) { return groups == 512 ? Deal<512>::first(w, units) : Deal<256>::first(w, units); }
+extern "C" int pair_cost() { return kAttendPairCost; }
 """
 
 
+def plan_library():
+    lib = host_library(PLAN)
+    i, q = ctypes.c_int, ctypes.c_int64
+    lib.workers.restype, lib.workers.argtypes = q, [i, q]
+    lib.first.restype, lib.first.argtypes = q, [i, q, q]
+    return lib
+
+
+@pytest.mark.parametrize("groups", [256, 512])
+def test_units_are_dealt_out_evenly(groups):
+    """Every unit has one worker, no worker is without a unit, and none has more than the even share rounded up (the few that there
+    are in a small call: two)."""
+    lib = plan_library()
+    rng = random.Random(groups)
+    for total in [1, 2, 3, 255, 1023, 1024, 1025, 2047, 2048, 4095, 4096, 4097, 2 ** 31 - 1] + [rng.randint(1, 20000) for _ in range(40)]:
+        n = lib.workers(groups, total)
+        assert 1 <= n <= min(total, 4 * groups)
+        firsts = [lib.first(groups, w, total) for w in range(n + 1)]
+        sizes = [b - a for a, b in zip(firsts, firsts[1:])]
+        assert firsts[0] == 0 and firsts[-1] == total and min(sizes) >= 1 and max(sizes) <= max(2, -(-total // (4 * groups)))
+        assert lib.first(groups, n, total) == lib.first(groups, 4 * groups, total) == total
+
+
 @pytest.mark.parametrize("seed", range(4))
-def test_the_grid_holds_every_share(seed):
-    """Whatever the lengths: the workgroups that the videos' rows ask for are at most the grid, a call that is not joined has one per
-    pair, and the parts of the workspace lie one behind the other."""
-    lib = host_library("#include <initializer_list>\n" + PLAN)
-    lib.tiles_per_group.restype = ctypes.c_int64
+def test_partial_results_have_slots_of_their_own(seed):
+    """Whatever the lengths, as the kernel goes through them: every tile has one worker, two parts of results never share a slot, all slots
+    are in the workspace, calls that are not joined have no parts, and the regions of the workspace lie one behind the other."""
+    lib = plan_library()
+    cost = lib.pair_cost()
     rng = random.Random(seed)
-    for _ in range(400):
+    for _ in range(60):
         Hq, Hkv = rng.choice([(28, 4), (40, 40), (71, 1), (17, 1), (8, 8), (1, 1), (1024, 2)])
-        Bn = rng.choice([1, 2, 8, 64, 65, 500, 4096])
-        esize, dh = rng.choice([(2, 128), (4, 64), (2, 256)])
-        cap = int(2 ** rng.uniform(0, 18))
+        Bn = rng.choice([1, 2, 8, 64, 65, 300])
+        esize, dh = rng.choice([(2, 128), (4, 64), (2, 256), (2, 32), (4, 32)])
+        cap = int(2 ** rng.uniform(0, 13))
         w = rng.randint(0, 1)
-        o = (ctypes.c_int64 * 12)()
+        o = (ctypes.c_int64 * 15)()
         lib.attend_plan(Bn, Hq, Hkv, ctypes.c_int64(cap), dh, esize, w, o)
-        tile, row_blocks, rows, pairs, grid, joined, stride, ml, part, lse2, logits, total = list(o)
+        tile, row_blocks, rows, pairs, grid, most_workers, joined, stride, table, ml, part, lse2, logits, total, groups = list(o)
         heads = Hkv * row_blocks
-        assert pairs == Bn * heads and row_blocks * 16 >= Hq // Hkv > (row_blocks - 1) * 16
+        assert pairs == Bn * heads and row_blocks * 16 >= Hq // Hkv > (row_blocks - 1) * 16 and most_workers == 4 * groups
+        slots = (part - ml) // (rows * 2 * 4)
         for kind in range(4):
             fresh = rng.randint(0, 1)
             lens = [cap if kind == 0 else (0 if kind == 1 else rng.randint(0, cap) if kind == 2 or rng.random() < 0.02 else min(cap, 3)) for _ in range(Bn)]
-            tiles = [-(-(n + fresh) // tile) for n in lens]
-            per = lib.tiles_per_group(ctypes.c_int64(sum(tiles) * heads))
-            splits = [max(1, -(-t // per)) for t in tiles]
-            assert sum(splits) * heads <= grid
-            assert joined or max(splits) == 1
-            assert all(s <= max(t, 1) for s, t in zip(splits, tiles))
+            tiles = [max(1, -(-(n + fresh) // tile)) for n in lens]
+            units = sum(t + cost for t in tiles) * heads
+            n = lib.workers(groups, units)
+            # workers are spread over the workgroups first: worker = wave * grid + workgroup
+            assert n <= 4 * grid and (grid == groups or n <= grid)
+            firsts = [lib.first(groups, x, units) for x in range(n + 1)]
+            used, at, x = set(), 0, 0
+            for t in tiles:
+                for _ in range(heads):
+                    mine = set()
+                    for unit in range(at, at + t):
+                        while firsts[x + 1] <= unit:
+                            x += 1
+                        mine.add(x)
+                    mine = sorted(mine)
+                    assert mine == list(range(mine[0], mine[-1] + 1))
+                    if len(mine) > 1:
+                        assert joined
+                        mine = [2 * v + (v == mine[0]) for v in mine]
+                        assert not used & set(mine) and max(mine) < slots
+                        used |= set(mine)
+                    at += t + cost
+        if joined or w:
+            assert ml - table >= pairs * 8
         if joined:
-            assert part - ml >= grid * rows * 2 * 4 and lse2 - part >= grid * rows * dh * 4
+            assert lse2 - part >= slots * rows * dh * 4
         if w:
             assert stride >= cap + 1 and stride % 32 == 0 and logits - lse2 >= Bn * Hq * 4 and total - logits == -(-Bn * Hq * stride * 4 // 256) * 256
         else:
