@@ -85,8 +85,13 @@ struct LengthTable { int n; int32_t len[METOK_MAX_LAYERS]; };
 
 RowMoveGeom row_move_geom(int64_t row_bytes);
 size_t row_move_workspace_bytes(int L, int B, int Hkv, int n_which, int64_t S_cap, int64_t row_bytes);
-// A launch that takes the place of the mover's own first one: it clears the words before the moves and may write the index lists.
-struct RowMoveStart { int (*launch)(void* context, uint32_t* words, size_t n_words, hipStream_t st); void* context; };
+// A launch that takes the place of the mover's own first one: it clears the words before the moves and writes the index lists and, in
+// `moved`, the tiles of every (layer, video) that have rows to move: the first one, and how many from there on.
+struct RowMoveStart {
+    int (*launch)(void* context, uint32_t* words, size_t n_words, hipStream_t st);
+    void* context;
+    const int2* moved;               // [L, B]
+};
 int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_which, int64_t S_cap, int64_t row_bytes,
                      const int32_t* page_table, int page_size, int pages_per_seq, int64_t n_pages_pool,
                      int32_t* new_len, const int32_t* host_len, int L_total,

@@ -14,7 +14,7 @@
 namespace metok {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64;
-constexpr int kEvictCache = 40;                                // weights a thread holds
+constexpr int kEvictCache = 40, kEvictFew = 8;                  // weights a thread holds
 constexpr int kEvictBins = 2048, kEvictDigit = 11;
 constexpr int kEvictList = 512;                                // keys that are ranked against each other
 
@@ -27,6 +27,8 @@ struct EvictArgs {
     int32_t* new_len;                                          // [L, B]
     int64_t weight_stride;
     int B, select_blocks, S_cap, n_first, n_last;
+    int2* moved;                                               // [L, B] or NULL: the row mover's tiles (see RowMoveStart)
+    int rows_per_tile;
     uint32_t* clear;                                           // words that the workgroups behind the selecting ones clear
     uint64_t n_clear;
 };
@@ -38,11 +40,12 @@ struct EvictShared {
     int scan[17];
     uint32_t low[kEvictWaves], high[kEvictWaves];
     int above[kEvictWaves], equal[kEvictWaves];
-    int bucket, need, count, n_list;
+    int bucket, need, count, n_list, first_moved;
     uint32_t tau;
 };
 
-template <bool CACHED>
+// CACHE: weights a thread holds, 0: none.
+template <int CACHE>
 __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const EvictArgs a) {
     __shared__ EvictShared s;
     if (static_cast<int>(blockIdx.x) >= a.select_blocks) {
@@ -55,7 +58,10 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
     const float* weight = a.weight[layer];                     // may be weight_out
     const int held = a.len[blockIdx.x], n = held < 0 ? 0 : (held > a.S_cap ? a.S_cap : held);
     const int budget = a.budget[layer];
-    if (tid == 0) a.new_len[blockIdx.x] = weight && n > budget ? budget : n;
+    if (tid == 0) {
+        a.new_len[blockIdx.x] = weight && n > budget ? budget : n;
+        if (a.moved && (!weight || n <= budget)) a.moved[blockIdx.x] = make_int2(0, 0);
+    }
     if (!weight) return;
     weight += static_cast<int64_t>(b) * a.weight_stride;
     float* weight_out = a.weight_out[layer] + static_cast<int64_t>(b) * a.weight_stride;
@@ -69,25 +75,23 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
 
     const int lo = a.n_first, hi = n - a.n_last;               // the rows between are ranked; lo < hi since budget < n
     const int per_wave = ((n + kEvictWaves - 1) / kEvictWaves + 63) & ~63;
-    const int base = wave * per_wave, steps = per_wave >> 6;
-    float held_w[CACHED ? kEvictCache : 1];
-    if constexpr (CACHED) {
+    const int base = wave * per_wave + lane, steps = per_wave >> 6;        // the lane's rows are base, base + 64, ...
+    float own[CACHE ? CACHE : 1];
+    if constexpr (CACHE != 0) {
 #pragma unroll
-        for (int i = 0; i < kEvictCache; ++i)
-            if (i < steps) held_w[i] = weight[min(base + i * 64 + lane, n - 1)];
+        for (int i = 0; i < CACHE; ++i) own[i] = weight[min(base + (i < steps ? i : 0) * 64, n - 1)];
     }
     // visit(key) for the rows that are ranked
     auto for_each = [&](auto visit) {
-        if constexpr (CACHED) {
+        if constexpr (CACHE != 0) {
 #pragma unroll
-            for (int i = 0; i < kEvictCache; ++i)
-                if (i < steps) {
-                    const int j = base + i * 64 + lane;
-                    if (j >= lo && j < hi) visit(ordered_key(held_w[i]));
-                }
+            for (int i = 0; i < CACHE; ++i) {
+                const int j = base + i * 64;
+                if (i < steps && j >= lo && j < hi) visit(ordered_key(own[i]));
+            }
         } else {
             for (int i = 0; i < steps; ++i) {
-                const int j = base + i * 64 + lane;
+                const int j = base + i * 64;
                 if (j >= lo && j < hi) visit(ordered_key(weight[j]));
             }
         }
@@ -97,13 +101,16 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
     int need = budget - a.n_first - a.n_last;                  // 0 <= need < hi - lo
     uint32_t tau = 0xffffffffu;
     int equal_kept = 0;
-    if (need > 0) {
+    const bool ranked_stay = need > 0;
+    if (ranked_stay) {
         uint32_t kmin = 0xffffffffu, kmax = 0u;
         for_each([&](uint32_t k) { kmin = min(kmin, k); kmax = max(kmax, k); });
         kmin = wave_extreme<false>(kmin);
         kmax = wave_extreme<true>(kmax);
         if (lane == 0) { s.low[wave] = kmin; s.high[wave] = kmax; }
-        __syncthreads();
+        s.hist[tid] = 0; s.hist[tid + kEvictThreads] = 0;
+        if (tid == 0) s.n_list = 0;
+        lds_barrier();
         kmin = wave_extreme<false>(s.low[lane & (kEvictWaves - 1)]);
         kmax = wave_extreme<true>(s.high[lane & (kEvictWaves - 1)]);
         const uint32_t range = kmax - kmin;
@@ -112,8 +119,6 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
         int count = hi - lo;                                               // rows that share them
         while (top > 0 && count > kEvictList) {
             const int bits = min(top, kEvictDigit), shift = top - bits;
-            s.hist[tid] = 0; s.hist[tid + kEvictThreads] = 0;
-            __syncthreads();
             // a run of equal digits costs a thread one addition: weights that were never raised are all the same
             int digit = -1, run = 0;
             for_each([&](uint32_t k) {
@@ -128,14 +133,15 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
                 }
             });
             if (run) atomicAdd(&s.hist[digit], run);
-            __syncthreads();
-            // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t
+            lds_barrier();
+            // from the top: thread t has bins 2047 - 2 t and 2046 - 2 t, and leaves them empty
             const int b0 = kEvictBins - 1 - 2 * tid, v0 = s.hist[b0], v1 = s.hist[b0 - 1];
+            s.hist[b0] = 0; s.hist[b0 - 1] = 0;
             int all;
             const int before = block_exclusive_scan_lds(v0 + v1, s.scan, &all);
             if (before < need && before + v0 >= need) { s.bucket = b0; s.need = need - before; s.count = v0; }
             else if (before + v0 < need && before + v0 + v1 >= need) { s.bucket = b0 - 1; s.need = need - before - v0; s.count = v1; }
-            __syncthreads();
+            lds_barrier();
             prefix = (top >= 32 ? 0u : prefix << bits) | static_cast<uint32_t>(s.bucket);
             need = s.need; count = s.count;
             top = shift;
@@ -144,12 +150,10 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
             tau = kmin + prefix;
             equal_kept = need;
         } else {
-            if (tid == 0) s.n_list = 0;
-            __syncthreads();
             for_each([&](uint32_t k) {
                 if (top >= 32 || ((k - kmin) >> top) == prefix) s.list[atomicAdd(&s.n_list, 1)] = k;      // count of them, at most kEvictList
             });
-            __syncthreads();
+            lds_barrier();
             if (tid < count) {
                 const uint32_t k = s.list[tid];
                 int above = 0, equal = 0;
@@ -161,47 +165,54 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
                 }
                 if (above < need && above + equal >= need) { s.tau = k; s.need = need - above; }       // equal keys write the same
             }
-            __syncthreads();
+            lds_barrier();
             tau = s.tau;
             equal_kept = s.need;
         }
     }
+    if (tid == 0) s.first_moved = 0x7fffffff;                  // behind a barrier below
 
     // Places.  A row stays if it is not ranked, above tau, or among the first equal_kept rows equal to tau.
     auto kind = [&](int j, float w, bool& above, bool& equal) {
         const bool in = j < n, ranked = j >= lo && j < hi;
         const uint32_t k = ordered_key(w);
-        above = in && (!ranked || (a.budget[layer] > a.n_first + a.n_last && k > tau));
+        above = in && (!ranked || (ranked_stay && k > tau));
         equal = in && ranked && k == tau;
     };
-    if constexpr (CACHED) {
+    const unsigned long long below = (1ull << lane) - 1;
+    int moved = 0x7fffffff;                                    // first place of this wave that takes a row from behind it
+    if constexpr (CACHE != 0) {
+        // the kinds of the lane's rows as bits: asked for twice
+        unsigned long long is_above = 0, is_equal = 0;
         int above_here = 0, equal_here = 0;
 #pragma unroll
-        for (int i = 0; i < kEvictCache; ++i)
+        for (int i = 0; i < CACHE; ++i)
             if (i < steps) {
                 bool above, equal;
-                kind(base + i * 64 + lane, held_w[i], above, equal);
+                kind(base + i * 64, own[i], above, equal);
+                is_above |= static_cast<unsigned long long>(above) << i;
+                is_equal |= static_cast<unsigned long long>(equal) << i;
                 above_here += __popcll(__ballot(above));
                 equal_here += __popcll(__ballot(equal));
             }
         if (lane == 0) { s.above[wave] = above_here; s.equal[wave] = equal_here; }
         __syncthreads();                                                   // all weights are in registers: weight_out may be weight
-        int place = 0, equals = 0;
-        for (int w = 0; w < wave; ++w) { place += s.above[w]; equals += s.equal[w]; }
-        place += min(equals, equal_kept);
+        const int sums_above = row16_inclusive_scan(s.above[lane & 15]), sums_equal = row16_inclusive_scan(s.equal[lane & 15]);
+        int equals = __builtin_amdgcn_readlane(sums_equal, wave) - equal_here;
+        int place = __builtin_amdgcn_readlane(sums_above, wave) - above_here + min(equals, equal_kept);
 #pragma unroll
-        for (int i = 0; i < kEvictCache; ++i)
+        for (int i = 0; i < CACHE; ++i)
             if (i < steps) {
-                const int j = base + i * 64 + lane;
-                bool above, equal;
-                kind(j, held_w[i], above, equal);
-                const unsigned long long eq = __ballot(equal), below = (1ull << lane) - 1;
-                const bool stays = above || (equal && equals + __popcll(eq & below) < equal_kept);
+                const int j = base + i * 64;
+                const bool equal = (is_equal >> i) & 1ull;
+                const unsigned long long eq = __ballot(equal);
+                const bool stays = ((is_above >> i) & 1ull) || (equal && equals + __popcll(eq & below) < equal_kept);
                 const unsigned long long st = __ballot(stays);
+                const int at = place + __popcll(st & below);
                 if (stays) {
-                    const int at = place + __popcll(st & below);
                     idx[at] = j;
-                    weight_out[at] = held_w[i];
+                    weight_out[at] = own[i];
+                    if (at != j) moved = min(moved, at);
                 }
                 place += __popcll(st);
                 equals += __popcll(eq);
@@ -214,7 +225,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
             const float w = weight[min(j, n - 1)];
             bool above, equal;
             kind(j, w, above, equal);
-            const unsigned long long eq = __ballot(equal), ab = __ballot(above), below = (1ull << lane) - 1;
+            const unsigned long long eq = __ballot(equal), ab = __ballot(above);
             __syncthreads();
             if (lane == 0) { s.above[wave] = __popcll(ab); s.equal[wave] = __popcll(eq); }
             __syncthreads();
@@ -228,9 +239,21 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
                 const int at = place + above_before + __popcll(ab & below) + (min(equal_rank, equal_kept) - min(equals, equal_kept));
                 idx[at] = j;
                 weight_out[at] = w;
+                if (at != j) moved = min(moved, at);
             }
             place += above_all + (min(equals + equal_all, equal_kept) - min(equals, equal_kept));
             equals += equal_all;
+        }
+        __syncthreads();
+    }
+    if (a.moved) {
+        const int first = static_cast<int>(wave_extreme<false>(static_cast<uint32_t>(moved)));
+        if (lane == 0 && first != 0x7fffffff) atomicMin(&s.first_moved, first);
+        lds_barrier();
+        if (tid == 0) {
+            const int tile = s.first_moved == 0x7fffffff ? 0 : s.first_moved / a.rows_per_tile;
+            const int tiles = s.first_moved == 0x7fffffff ? 0 : (budget + a.rows_per_tile - 1) / a.rows_per_tile - tile;
+            a.moved[blockIdx.x] = make_int2(tile, tiles);
         }
     }
 }
@@ -240,8 +263,9 @@ static int launch_select(EvictArgs& a, int L, uint32_t* clear, size_t n_clear, h
     a.select_blocks = L * a.B;
     const size_t blocks = (n_clear + kEvictThreads * 4 - 1) / (kEvictThreads * 4);
     const dim3 grid(static_cast<unsigned>(a.select_blocks + (blocks < 256 ? blocks : 256)));
-    if (a.S_cap <= kEvictCache * kEvictThreads) hipLaunchKernelGGL(evict_select_kernel<true>, grid, dim3(kEvictThreads), 0, st, a);
-    else hipLaunchKernelGGL(evict_select_kernel<false>, grid, dim3(kEvictThreads), 0, st, a);
+    if (a.S_cap <= kEvictFew * kEvictThreads) hipLaunchKernelGGL(evict_select_kernel<kEvictFew>, grid, dim3(kEvictThreads), 0, st, a);
+    else if (a.S_cap <= kEvictCache * kEvictThreads) hipLaunchKernelGGL(evict_select_kernel<kEvictCache>, grid, dim3(kEvictThreads), 0, st, a);
+    else hipLaunchKernelGGL(evict_select_kernel<0>, grid, dim3(kEvictThreads), 0, st, a);
     return check_launch("evict select");
 }
 
@@ -273,14 +297,18 @@ static int select_args(EvictArgs* a, const float* const* weight, float* const* w
         a->weight_out[l] = o; a->idx[l] = idx[l]; a->budget[l] = budget[l];
     }
     a->len = len; a->new_len = new_len; a->weight_stride = weight_stride;
+    a->moved = nullptr; a->rows_per_tile = 1;
     a->B = B; a->S_cap = static_cast<int>(S_cap); a->n_first = n_first; a->n_last = n_last;
     return METOK_OK;
 }
 
-// What the row mover runs in place of its own start: the selection clears the mover's words, too.
-struct SelectStart { EvictArgs* args; int L; };
+static size_t moved_bytes(int L, int B) { return round_up(static_cast<size_t>(L) * B * sizeof(int2), 256); }
+
+// What the row mover runs in place of its own start, all other arguments checked: the selection clears the mover's words, too.
+struct SelectStart { EvictArgs* args; int L; size_t workspace_bytes, need; };
 static int start_with_selection(void* context, uint32_t* words, size_t n_words, hipStream_t st) {
     const SelectStart* s = static_cast<const SelectStart*>(context);
+    if (s->workspace_bytes < s->need) return fail(METOK_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", s->need, s->workspace_bytes);
     return launch_select(*s->args, s->L, words, n_words, st);
 }
 
@@ -291,8 +319,13 @@ static int evict_impl(void* const* k, void* const* v, int L, int B, int Hkv, int
     EvictArgs a;
     int rc = select_args(&a, weight, weight_out, weight_stride, L, B, S_cap, len, budget, n_first, n_last, idx, new_len);
     if (rc) return rc;
-    SelectStart context{&a, L};
-    const RowMoveStart start{start_with_selection, &context};
+    const size_t mover = metok_kv_compact_workspace_bytes(L, B, Hkv, S_cap, dh, dtype);        // 0: the mover refuses the shape below
+    if (mover) {
+        a.moved = reinterpret_cast<int2*>(static_cast<char*>(workspace) + mover);
+        a.rows_per_tile = row_move_geom(static_cast<int64_t>(dh) * static_cast<int64_t>(dtype_size(dtype))).rows_per_tile;
+    }
+    SelectStart context{&a, L, workspace_bytes, mover + moved_bytes(L, B)};
+    const RowMoveStart start{start_with_selection, &context, a.moved};
     return compact_layers(k, v, L, B, Hkv, S_cap, dh, dtype, a.idx, a.budget, nullptr, page_table, page_size, pages_per_seq, n_pages,
                           workspace, workspace_bytes, stream, &start);
 }
@@ -303,7 +336,8 @@ using namespace metok;
 
 extern "C" size_t metok_kv_evict_workspace_bytes(int L, int B, int Hkv, int64_t S_cap, int dh, int dtype) {
     if (B > METOK_MAX_DECODE_BATCH || S_cap > INT32_MAX - 4096) return 0;
-    return metok_kv_compact_workspace_bytes(L, B, Hkv, S_cap, dh, dtype);
+    const size_t mover = metok_kv_compact_workspace_bytes(L, B, Hkv, S_cap, dh, dtype);
+    return mover ? mover + moved_bytes(L, B) : 0;
 }
 
 extern "C" int metok_kv_evict(void* const* k_layers, void* const* v_layers, int L, int B, int Hkv, int64_t S_cap, int dh, int dtype,

@@ -85,6 +85,8 @@ struct MoveArgs {
     // first_item / n_sub + video * tiles + tile, ascending within a (layer, video); *n_work of them
     const int32_t* worklist;
     const uint32_t* n_work;
+    // listed variant only: first tile and tiles with rows to move of every [layer, video] (by layer_id)
+    const int2* moved;
 };
 
 enum { kMoveDense = 0, kMovePaged = 1, kMoveRelink = 2 };
@@ -111,7 +113,11 @@ __device__ __forceinline__ int wave_lower_bound(const int32_t* __restrict__ idx,
     return lo;
 }
 
-template <int MODE>
+// LISTED: the tiles of args.moved alone, in the same order.  Every workgroup takes a ticket; while it is on its way the tiles before each
+// (layer, video) are counted, and those whose ticket lies behind the last tile leave.  They are the last ones to start: with eight videos of which
+// two have rows to move the others' tiles, which each took a turn on a CU to find that out, were three quarters of them (28 layers of pages of 16
+// rows, 2 of 8 videos 4096 -> 2048 rows: ORD).
+template <int MODE, bool LISTED = false>
 __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs args) {
     constexpr bool PAGED = MODE != kMoveDense;
     constexpr int U = kMoveInFlight;
@@ -125,6 +131,26 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
         const int g = blockIdx.x & (args.n_tickets - 1);
         s_item = static_cast<int>(atomicAdd(args.ticket + g * kTicketStride, 1u)) * args.n_tickets + g;
     }
+    int slot = 0, b, tile, sub;
+    if constexpr (LISTED) {
+        __shared__ int s_scan[17], s_group, s_tile;
+        if (threadIdx.x == 0) s_group = -1;
+        const int n_groups = args.n_layers * args.B;
+        for (int base = 0, done = 0; base < n_groups; base += kMoveThreads) {
+            const int g = base + static_cast<int>(threadIdx.x), of = g / args.B;
+            const int2 m = g < n_groups ? args.moved[static_cast<int64_t>(args.layer[of].layer_id) * args.B + (g - of * args.B)] : make_int2(0, 0);
+            int here = 0;
+            const int before = done + block_exclusive_scan(m.y, s_scan, &here), want = s_item / n_sub;
+            if (want >= before && want < before + m.y) { s_group = g; s_tile = m.x + want - before; }
+            done += here;
+        }
+        __syncthreads();
+        if (s_group < 0) return;
+        slot = s_group / args.B;
+        b = s_group - slot * args.B;
+        tile = s_tile;
+        sub = s_item % n_sub;
+    } else {
     __syncthreads();
     int item = s_item;
     if (item >= n_items) return;
@@ -132,15 +158,16 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
         const int k = item / n_sub;
         item = args.worklist[k] * n_sub + (item - k * n_sub);
     }
-    int slot = 0;
     while (slot + 1 < args.n_layers && args.layer[slot + 1].first_item <= item) ++slot;
-    const RowMoveLayer& L = args.layer[slot];
     // item -> (video, tile, sub-slab): the sub-slabs of one video share its index list and advance together
-    const int local = item - L.first_item;
-    const int b = local / (n_sub * L.tiles);
-    int rem = local - b * n_sub * L.tiles;
-    const int tile = rem / n_sub;
-    int sub = rem - tile * n_sub;
+    const int local = item - args.layer[slot].first_item;
+    b = local / (n_sub * args.layer[slot].tiles);
+    const int rem = local - b * n_sub * args.layer[slot].tiles;
+    tile = rem / n_sub;
+    sub = rem - tile * n_sub;
+    }
+    const RowMoveLayer& L = args.layer[slot];
+    const int sub_slab = sub;
     const int part = sub % args.parts; sub /= args.parts;
     const int which = sub % args.n_which;
     const int head = sub / args.n_which;
@@ -153,7 +180,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
                                                     static_cast<int64_t>(b) * args.pages_per_seq : nullptr;
     const int64_t lb = (static_cast<int64_t>(L.layer_id) * args.B + b) * args.pages_per_seq;
     const int32_t* __restrict__ table_dst = MODE == kMoveRelink ? args.table_out + lb : table;
-    uint32_t* flags = args.flags + (static_cast<size_t>(L.flag_slot) * args.B * n_sub + static_cast<size_t>(b) * n_sub + (rem - tile * n_sub)) *
+    uint32_t* flags = args.flags + (static_cast<size_t>(L.flag_slot) * args.B * n_sub + static_cast<size_t>(b) * n_sub + sub_slab) *
                                        args.tiles_max;
 
     const int lpr = args.lanes_per_row;
@@ -554,9 +581,14 @@ int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_w
         args.home_page = relink ? relink->home_page : nullptr;
         args.worklist = relink ? relink->plan->worklist + static_cast<int64_t>(launch) * kMaxLayersPerLaunch * B * tiles_max : nullptr;
         args.n_work = relink ? words + 1 + n_launches + launch : nullptr;
+        args.moved = start ? start->moved : nullptr;
         if (items == 0) continue;
         if (relink)
             { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL(move_rows_kernel<kMoveRelink>, dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
+        else if (start && page_table)
+            { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL((move_rows_kernel<kMovePaged, true>), dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
+        else if (start)
+            { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL((move_rows_kernel<kMoveDense, true>), dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
         else if (page_table)
             { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL(move_rows_kernel<kMovePaged>, dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
         else
