@@ -512,11 +512,10 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
 }
 
 constexpr int kJoinThreads = 256;
-constexpr int kWeightRows = 256;       // cache rows a workgroup adds up at a time: four to a lane
+constexpr int kWeightRows = kJoinThreads;       // cache rows a workgroup adds up at a time: four to a lane
 // Up to so many workgroups a head's elements are spread over several of them, 32 each: with few heads every one has many parts (one
 // video of 2307 rows, 28 heads: 10.1 us a call with one workgroup a head, 9.0 with four).
 constexpr int kJoinSpread = 512;
-
 // (m, l) stands for the sum l 2^m.
 __device__ __forceinline__ void add_sum(float& m, float& l, float m2, float l2) {
     const float to = fmaxf(m, m2), ref = to == -INFINITY ? 0.f : to;
@@ -565,9 +564,9 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
             const float2 v = ml[parts.slot(p)];
             add_sum(m, l, v.x, v.y);
         }
-#pragma unroll
-        for (int off = 32; off; off >>= 1) add_sum(m, l, __shfl_xor(m, off, 64), __shfl_xor(l, off, 64));
-        const float lse2 = l == 0.f ? INFINITY : m + log2_of(l);            // +inf, no row counts: the factors below are 0
+        const float top = score_of_key(wave_extreme<true>(ordered_key(m))), ref = top == -INFINITY ? 0.f : top;
+        l = wave_sum(l * exp2_of(m - ref));
+        const float lse2 = l == 0.f ? INFINITY : ref + log2_of(l);            // +inf, no row counts: the factors below are 0
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         auto add = [&](const float4& v, float f) { o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w); };
 #pragma unroll
@@ -607,7 +606,7 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
         const int h = min(h0 + static_cast<int>(threadIdx.x) / a.head_lanes, a.Hq - 1), part = threadIdx.x % a.head_lanes;
         const HeadParts parts = parts_of(a, b, h);
         float m = -INFINITY, l = 0.f;
-#pragma unroll 4
+#pragma unroll 8
         for (int p = part; p < (parts.n > 1 ? parts.n : 0); p += a.head_lanes) {
             const float2 v = ml[parts.slot(p)];
             add_sum(m, l, v.x, v.y);
@@ -665,12 +664,13 @@ static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) 
     int rc = check_launch("decode attention");
     if (rc) return rc;
     const int64_t units = plan.joined ? static_cast<int64_t>(a.B) * a.Hq : 0;
-    const int64_t weight_blocks = a.weight ? static_cast<int64_t>(a.B) * a.weight_blocks : 0;
     // few heads have many parts each: their elements over several workgroups
     a.join_lanes = units * (DH / 4 / 8) <= kJoinSpread ? 8 : DH / 4;
     a.join_blocks = static_cast<int>(units * (DH / 4 / a.join_lanes));
-    const int64_t blocks = a.join_blocks + weight_blocks;
+    const int64_t blocks = a.join_blocks + (a.weight ? static_cast<int64_t>(a.B) * a.weight_blocks : 0);
     if (blocks == 0) return METOK_OK;
+    a.head_lanes = 64;
+    while (a.head_lanes > 1 && a.Hq * a.head_lanes > kJoinThreads) a.head_lanes /= 2;
     hipLaunchKernelGGL((decode_join_kernel<T, DH>), dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads), 0, st, a);
     return check_launch("decode join");
 }
@@ -743,8 +743,6 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
     // every workgroup of the weights sums up the heads' shares for itself: enough of them for the chip, not more
     const int64_t most = (S_cap + kWeightRows - 1) / kWeightRows, enough = (1024 + B - 1) / B;
     a.weight_blocks = static_cast<int>(most < enough ? most : enough);
-    a.head_lanes = 64;
-    while (a.head_lanes > 1 && Hq * a.head_lanes > kJoinThreads) a.head_lanes /= 2;
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (dtype == METOK_BF16) {
         if (dh == 32) return launch_attend<bf16_t, 32>(a, plan, st);

@@ -113,10 +113,10 @@ __device__ __forceinline__ int wave_lower_bound(const int32_t* __restrict__ idx,
     return lo;
 }
 
-// LISTED: the tiles of args.moved alone, in the same order.  Every workgroup takes a ticket; while it is on its way the tiles before each
-// (layer, video) are counted, and those whose ticket lies behind the last tile leave.  They are the last ones to start: with eight videos of which
-// two have rows to move the others' tiles, which each took a turn on a CU to find that out, were three quarters of them (28 layers of pages of 16
-// rows, 2 of 8 videos 4096 -> 2048 rows: ORD).
+// LISTED: the tiles of args.moved alone, in the same order.  A workgroup takes one ticket after the other, and while a ticket is on its way the tiles
+// before each (layer, video) are counted; a ticket behind the last tile ends it.  With a turn for every tile of the cache the tiles of videos
+// that stay as they are, three quarters of them, each held a place on a CU to find that out (2 of 8 videos beyond the budget: 260 us).
+// A tile waits only for tiles of earlier tickets, whose workgroups hold no later one: the waits end as above.
 template <int MODE, bool LISTED = false>
 __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs args) {
     constexpr bool PAGED = MODE != kMoveDense;
@@ -127,6 +127,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
     // each, the others leave before they touch the counter.
     const int64_t n_items = MODE == kMoveRelink ? static_cast<int64_t>(*args.n_work) * n_sub : args.total_items;
     if (MODE == kMoveRelink && static_cast<int64_t>(blockIdx.x) >= n_items) return;
+    for (bool more = true; more; more = LISTED) {
     if (threadIdx.x == 0) {
         const int g = blockIdx.x & (args.n_tickets - 1);
         s_item = static_cast<int>(atomicAdd(args.ticket + g * kTicketStride, 1u)) * args.n_tickets + g;
@@ -294,6 +295,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
 #pragma unroll
     for (int u = 0; u < U; ++u)
         if (dst[u] != nullptr) __builtin_nontemporal_store(v[u], reinterpret_cast<u32x4_t*>(dst[u]));
+    }
 }
 
 // Clears the words the move kernels will use (flags, tickets, error word) and writes the per-layer lengths.
@@ -498,6 +500,11 @@ size_t row_move_workspace_bytes(int L, int B, int Hkv, int n_which, int64_t S_ca
     return round_up((move_header_words(L) + flags) * sizeof(uint32_t), 256);
 }
 
+// Two workgroups to a CU: of the listed variant's tiles few may move, and a workgroup that starts only to find no tile takes 2 us of a place (two of
+// eight videos of 28 layers 4096 -> 2048 rows in pages: 130 us with a workgroup per tile of the cache, 106 with 512, 108 with 1024, 115 with 2048;
+// four videos 18560 -> 9280: 752, 740, 743, 749).
+static unsigned listed_groups(int64_t items) { return static_cast<unsigned>(items < 512 ? items : 512); }
+
 // Host side of both stage-3 calls and of the in-place hidden-state compaction.  layers[i] needs k (v if
 // n_which == 2), idx and n_keep; layers with n_keep == 0 must have been left out by the caller.
 int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_which, int64_t S_cap, int64_t row_bytes,
@@ -586,9 +593,9 @@ int launch_row_moves(RowMoveLayer* layers, int n_active, int B, int Hkv, int n_w
         if (relink)
             { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL(move_rows_kernel<kMoveRelink>, dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
         else if (start && page_table)
-            { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL((move_rows_kernel<kMovePaged, true>), dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
+            { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL((move_rows_kernel<kMovePaged, true>), dim3(listed_groups(items)), dim3(kMoveThreads), 0, st, args); }
         else if (start)
-            { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL((move_rows_kernel<kMoveDense, true>), dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
+            { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL((move_rows_kernel<kMoveDense, true>), dim3(listed_groups(items)), dim3(kMoveThreads), 0, st, args); }
         else if (page_table)
             { TraceScope trace_scope(METOK_TRACE_MOVE_ROWS, st); hipLaunchKernelGGL(move_rows_kernel<kMovePaged>, dim3(static_cast<unsigned>(items)), dim3(kMoveThreads), 0, st, args); }
         else
