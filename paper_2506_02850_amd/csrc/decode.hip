@@ -336,10 +336,8 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
         if (a.cap > 0.f) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) s[i >> 2][i & 3] = a.cap * tanh_of(s[i >> 2][i & 3] * a.scale);
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) s[i >> 2][i & 3] *= a.scale;
         }
+        const float scale = a.cap > 0.f ? 1.f : a.scale;       // to the log2 domain, rounded once with the difference to the maximum
         if (!f.all) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -354,12 +352,12 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
         if (WEIGHTS && r < n_heads(x)) {
             float* to = a.logits + (static_cast<int64_t>(x.b) * a.Hq + first_head(x) + r) * a.logit_stride + x.t * TILE + 4 * c;
 #pragma unroll
-            for (int b = 0; b < NT; ++b) *reinterpret_cast<f32x4_t*>(to + 16 * b) = s[b];
+            for (int b = 0; b < NT; ++b) *reinterpret_cast<f32x4_t*>(to + 16 * b) = s[b] * scale;
         }
         float top = s[0][0];
 #pragma unroll
         for (int i = 1; i < NV; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-        top = rows_max(top);
+        top = rows_max(top) * scale;
         if (__any(top > m)) {
             const float to = fmaxf(m, top), g = exp2_of(m - (to == -INFINITY ? 0.f : to));
             m = to;
@@ -370,7 +368,7 @@ __global__ __launch_bounds__(kAttendThreads, 2) void decode_attention_kernel(con
         const float ref = m == -INFINITY ? 0.f : m;
         float p[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) { p[i] = exp2_of(s[i >> 2][i & 3] - ref); l += p[i]; }
+        for (int i = 0; i < NV; ++i) { p[i] = exp2_of(fmaf(s[i >> 2][i & 3], scale, -ref)); l += p[i]; }
         if constexpr (BF16) {
             // a probability is the sum of two bf16 numbers, 16 of its bits: with one, the result would be as far from the exact one
             // as its own rounding is once more; the second product hides in the wait for memory
