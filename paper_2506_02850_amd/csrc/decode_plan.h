@@ -7,7 +7,9 @@
 namespace metok {
 
 constexpr int kAttendWaves = 4, kAttendThreads = 64 * kAttendWaves;
-constexpr int kAttendRows = 16;                // query rows of a wave: one MFMA's columns
+constexpr int kAttendRows = 16;                // query rows of a block: one MFMA's columns
+// Blocks of a wave where a kv head has more than one: what fits the registers beside K, V and the sums.
+constexpr int attend_blocks(int dh) { return dh <= 64 ? 4 : 2; }
 // Cache rows of a tile: K and V of the next one are on their way in registers, 64 of them at most.
 constexpr int attend_tile(int esize, int dh) { return esize * dh <= 256 && esize == 2 ? 32 : 16; }
 // Workgroups of a large call: one per CU, two where a tile is only 4 KB (8 x 73980 rows of 4 heads of 32 bf16: 68 us with one, 57 with two, 57 with
@@ -35,7 +37,9 @@ template <int GROUPS> struct Deal {
 
 struct AttendPlan {
     int tile;              // cache rows of a tile
-    int row_blocks;        // blocks of kAttendRows query heads of a kv head
+    bool wide;             // several blocks of query heads of a kv head at a time
+    int block_rows;        // query heads of a kv head that are taken at a time, at most
+    int row_blocks;        // how often the rows are read for the query heads of a kv head
     int rows;              // query rows of a partial result
     int64_t pairs;         // (video, kv head, row block): what is split over the rows of the cache
     int64_t grid;          // workgroups
@@ -50,8 +54,10 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     AttendPlan p{};
     const int group = Hq / Hkv;
     p.tile = attend_tile(esize, dh);
-    p.row_blocks = (group + kAttendRows - 1) / kAttendRows;
-    p.rows = group < kAttendRows ? group : kAttendRows;
+    p.wide = group > kAttendRows;
+    p.block_rows = kAttendRows * (p.wide ? attend_blocks(dh) : 1);
+    p.row_blocks = (group + p.block_rows - 1) / p.block_rows;
+    p.rows = group < p.block_rows ? group : p.block_rows;
     p.pairs = static_cast<int64_t>(B) * Hkv * p.row_blocks;
     const int64_t most = (capacity + 1 + p.tile - 1) / p.tile;                       // tiles of the longest video
     p.joined = most > 1;
