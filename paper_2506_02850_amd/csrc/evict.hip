@@ -60,9 +60,10 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
     const float* weight = a.weight[layer];                     // may be weight_out
     const int held = a.len[blockIdx.x], n = held < 0 ? 0 : (held > a.S_cap ? a.S_cap : held);
     const int budget = a.budget[layer];
-    if (tid == 0) {
-        a.new_len[blockIdx.x] = weight && n > budget ? budget : n;
-        if (a.moved && (!weight || n <= budget)) a.moved[blockIdx.x] = make_int2(0, 0);
+    // new_len may be len: what replaces a larger number waits until all waves have read it (below)
+    if (tid == 0 && (!weight || n <= budget)) {
+        a.new_len[blockIdx.x] = n;
+        if (a.moved) a.moved[blockIdx.x] = make_int2(0, 0);
     }
     if (!weight) return;
     weight += static_cast<int64_t>(b) * a.weight_stride;
@@ -248,6 +249,7 @@ __global__ __launch_bounds__(kEvictThreads) void evict_select_kernel(const Evict
         }
         __syncthreads();
     }
+    if (tid == 0) a.new_len[blockIdx.x] = budget;             // behind a barrier that every wave reaches with n in use
     if (a.moved) {
         const int first = static_cast<int>(wave_extreme<false>(static_cast<uint32_t>(moved)));
         if (lane == 0 && first != 0x7fffffff) atomicMin(&s.first_moved, first);

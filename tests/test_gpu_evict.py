@@ -287,3 +287,19 @@ def test_refusals():
         B.metok_kv_evict(k, v, w, lens, 10, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     torch.cuda.synchronize()
     assert not w[0].any()
+
+
+@pytest.mark.parametrize("S", [96, 9000, 41000])
+def test_lengths_in_place_of_many_videos(S):
+    """new_len may be len: every wave of a video's workgroup has to see the old length."""
+    B = mk()
+    L, videos = (4, 1024) if S == 96 else (3, 40)
+    rng = np.random.default_rng(S)
+    w = [weights_of("attention", rng, (videos, S)) for _ in range(L)]
+    lens = rng.integers(S // 3, S + 1, (L, videos)).astype(np.int32)
+    budget = [S // 2 - 5 * l for l in range(L)]
+    lists, new = expected(w, lens, budget, 3, 11, S)
+    held = torch.from_numpy(lens).cuda()
+    res = B.metok_kv_evict_select([torch.from_numpy(x).cuda() for x in w], held, S, budget, 3, 11, new_len=held)
+    torch.cuda.synchronize()
+    check_selection(res, w, lists, new)
