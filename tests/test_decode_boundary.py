@@ -91,6 +91,18 @@ def test_refused_attention_calls(B):
     refused(-1, "overlaps", ws=FAKE[2], bytes=big)
 
 
+def test_scales_that_fp32_does_not_hold_are_refused(B):
+    """1e-40 would lose its bits, 1e-50 be 0: as a cap it would mean none, as a scale 0 times -inf where a row is not there."""
+    def refused(text, **kw):
+        assert B.lib().metok_decode_attention(*attention_args(**kw)) == -1, kw
+        assert text in B.metok_last_error(), (kw, B.metok_last_error())
+
+    for x in (1e-40, 1e-50, 5e-324, 1e30):
+        refused("scale must", scale=x)
+        refused("logit_cap must", cap=x)
+    refused("scale / logit_cap", scale=1e10, cap=1e-25)
+
+
 def test_refused_paged_attention_calls(B):
     f = B.lib().metok_decode_attention_paged
 
