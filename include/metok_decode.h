@@ -88,6 +88,8 @@ METOK_API int metok_decode_attention_paged(const void* q, int B, int Hq, int Hkv
  *                index lists of metok_kv_compact, _paged and metok_kv_relink_paged with n_keep[l] = budget[l].  A video within the budget has
  *                the list 0, 1, 2, ...: nothing of it moves.
  *   new_len      device out, [L, B] int32: min(len, budget[l]) (len where weight[l] is NULL); may be `len` itself.
+ *   Apart from the two cases named (weight_out[l] as weight[l], new_len as len) no output may overlap anything else that the call
+ *   reads or writes; of idx, weight, weight_out, len and new_len that is checked.
  * metok_kv_evict and metok_kv_evict_paged select and move the rows of the caches (row i <- row idx[l][b][i]; rows from
  * new_len on are left as they were); metok_kv_evict_select only selects, for callers that relink pages or move the rows themselves.
  *   workspace    metok_kv_evict_workspace_bytes() for the first two, none for the selection; as in metok_kv_compact its first word

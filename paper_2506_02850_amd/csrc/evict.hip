@@ -8,6 +8,8 @@
 // sixteenth of the rows, 64 neighbouring rows an instruction, so that the place of a kept row is a population count of lane
 // masks away from the number of rows that earlier waves keep: one exchange between the waves, no scan per tile.
 // What bounds it is latency: a video of 4224 rows is 17 KB, and some ten barriers and round trips to LDS take 6 us.
+#include <algorithm>
+
 #include "common.h"
 #include "metok_decode.h"
 
@@ -285,7 +287,15 @@ static int select_args(EvictArgs* a, const float* const* weight, float* const* w
     if (n_first < 0 || n_last < 0) return fail(METOK_ERR_INVALID_ARG, "n_first and n_last must not be negative");
     if (weight_stride < S_cap) return fail(METOK_ERR_INVALID_ARG, "weight_stride must be at least the capacity");
     const size_t lens = static_cast<size_t>(L) * B;
-    if (new_len != len && new_len < len + lens && len < new_len + lens) return fail(METOK_ERR_INVALID_ARG, "new_len overlaps len");
+    // what is read and written, by address: nothing written may overlap anything else
+    struct Span { uintptr_t from, to; bool written; } spans[3 * METOK_MAX_LAYERS + 2];
+    int n_spans = 0;
+    auto uses = [&](const void* p, size_t words, bool written) {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+        spans[n_spans++] = {from, from + 4 * words, written};
+    };
+    uses(new_len, lens, true);
+    if (len != new_len) uses(len, lens, false);
     const size_t span = static_cast<size_t>(B - 1) * weight_stride + S_cap;
     for (int l = 0; l < METOK_MAX_LAYERS; ++l) {
         a->weight[l] = l < L ? weight[l] : nullptr;
@@ -295,11 +305,21 @@ static int select_args(EvictArgs* a, const float* const* weight, float* const* w
         float* o = weight_out[l];
         if (!o || !idx[l] || ((reinterpret_cast<uintptr_t>(w) | reinterpret_cast<uintptr_t>(o) | reinterpret_cast<uintptr_t>(idx[l])) & 3u))
             return fail(METOK_ERR_INVALID_ARG, "layer %d: NULL or misaligned weight, weight_out or idx", l);
-        if (o != w && o < w + span && w < o + span) return fail(METOK_ERR_INVALID_ARG, "layer %d: weight_out overlaps weight", l);
         if (budget[l] < 1 || budget[l] > S_cap) return fail(METOK_ERR_INVALID_ARG, "budget[%d] = %d outside [1, capacity]", l, budget[l]);
         if (static_cast<int64_t>(n_first) + n_last > budget[l])
             return fail(METOK_ERR_INVALID_ARG, "n_first + n_last = %lld is more than budget[%d] = %d", static_cast<long long>(n_first) + n_last, l, budget[l]);
         a->weight_out[l] = o; a->idx[l] = idx[l]; a->budget[l] = budget[l];
+        uses(o, span, true);
+        if (o != w) uses(w, span, false);
+        uses(idx[l], static_cast<size_t>(B) * budget[l], true);
+    }
+    std::sort(spans, spans + n_spans, [](const Span& x, const Span& y) { return x.from < y.from; });
+    uintptr_t used = 0, written = 0;                           // ends of what lies before
+    for (int i = 0; i < n_spans; ++i) {
+        if (spans[i].from < (spans[i].written ? used : written))
+            return fail(METOK_ERR_INVALID_ARG, "one of weight_out, idx and new_len overlaps another of them, a weight that is not its own, or len");
+        used = std::max(used, spans[i].to);
+        if (spans[i].written) written = std::max(written, spans[i].to);
     }
     a->len = len; a->new_len = new_len; a->weight_stride = weight_stride;
     a->moved = nullptr; a->rows_per_tile = 1;

@@ -288,6 +288,34 @@ def test_refused_evictions(B):
     paged(-1, "capacity", page=2 ** 20, pps=2 ** 20)
 
 
+def test_evictions_whose_buffers_overlap_are_refused(B):
+    vp, i32 = ctypes.c_void_p, ctypes.c_int32
+    names = ("weight", "weight_out", "stride", "L", "B", "S_cap", "len", "budget", "first", "last", "idx", "new_len", "stream")
+
+    def refused(**kw):
+        a = evict_args(**kw)
+        assert B.lib().metok_kv_evict_select(*[a[n] for n in names]) == -1, kw
+        assert "overlaps" in B.metok_last_error(), (kw, B.metok_last_error())
+        assert B.lib().metok_kv_evict(*a.values()) == -1 and "overlaps" in B.metok_last_error()
+
+    same = (vp * 2)(FAKE[4], FAKE[4])
+    refused(weight=same, weight_out=same)                                # one buffer for two layers, in place
+    refused(weight_out=(vp * 2)(FAKE[6], FAKE[6] + 4 * 255))             # the second layer's from the last word of the first's
+    refused(weight_out=(vp * 2)(FAKE[5], FAKE[7]))                       # the first layer's onto the second's weights
+    refused(idx=(vp * 2)(FAKE[9], FAKE[9]))
+    refused(idx=(vp * 2)(FAKE[9], FAKE[9] + 4 * 127))
+    refused(idx=(vp * 2)(FAKE[4], FAKE[10]))
+    refused(idx=(vp * 2)(FAKE[9], FAKE[7] + 4))
+    refused(idx=(vp * 2)(FAKE[9], FAKE[8]))
+    refused(new_len=FAKE[10] + 4)
+    # neighbours, weights that two layers share, and layers without weights: no overlap; the workspace is what is missing
+    for kw in (dict(weight_out=(vp * 2)(FAKE[6], FAKE[6] + 4 * 256)), dict(idx=(vp * 2)(FAKE[9], FAKE[9] + 4 * 128)), dict(weight=same),
+               dict(weight=(vp * 2)(FAKE[4], None), weight_out=(vp * 2)(FAKE[6], FAKE[6]), idx=(vp * 2)(FAKE[9], FAKE[9])),
+               dict(weight_out=(vp * 2)(FAKE[4], FAKE[5])), dict(new_len=FAKE[8])):
+        a = evict_args(**kw)
+        assert B.lib().metok_kv_evict(*a.values()) == -3, (kw, B.metok_last_error())
+
+
 def test_eviction_workspace(B):
     f = B.metok_kv_evict_workspace_bytes
     assert f(28, 8, 4, 36992, 128, B.BF16) == B.metok_kv_compact_workspace_bytes(28, 8, 4, 36992, 128, B.BF16) + 28 * 8 * 8
