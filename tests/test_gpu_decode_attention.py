@@ -279,3 +279,55 @@ def test_refusals():
     with pytest.raises(B.MetokError):
         B.metok_decode_attention(q[:, :7].contiguous(), k, v, lens)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 32), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [0, 16, 7])
+@pytest.mark.parametrize("weights", [False, True])
+def test_every_kernel_of_many_query_heads(dtype, dh, page, weights):
+    """More than 16 query heads to a kv head: whole and part blocks, one and several turns of them."""
+    lens = [0, 1, 16, 31, 33, 260]
+    capacity = 350 if page == 0 else page * (-(-350 // page))
+    heads = [(71, 1), (64, 2), (65, 1), (34, 2), (128, 1), (48, 1), (66, 2)]
+    Hq, Hkv = heads[(dh // 32 + page + 3 * weights) % len(heads)]
+    run(C.make(dtype, lens, Hq, Hkv, dh, capacity, page, append=True, weights=weights, seed=dh + page))
+    run(C.make(dtype, lens, Hq, Hkv, dh, capacity, page, append=False, weights=weights, cap=20.0, seed=dh + page + 1))
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(32, 1), (33, 1), (64, 1), (71, 1), (1024, 1), (1024, 8), (512, 4)])
+def test_many_query_heads_split_and_joined(Hq, Hkv):
+    run(C.make("bf16", [2100 if Hq < 100 else 300, 5], Hq, Hkv, 64, 2112, 16, weights=True, seed=Hq))
+    run(C.make("f32", [40, 301], Hq, Hkv, 32, 320, append=False, seed=Hq + 1))
+
+
+def test_the_largest_batch():
+    """4096 videos, most of them short, in one call: 64 steps of the search for a worker's first video."""
+    rng = np.random.default_rng(12)
+    lens = rng.integers(0, 3, 4096)
+    lens[[0, 63, 64, 2000, 4095]] = [40, 0, 33, 40, 17]
+    run(C.make("f32", lens, 2, 1, 32, 40, weights=True, seed=12))
+
+
+@pytest.mark.parametrize("page", [1, 7, 8, 48])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (71, 1)])
+def test_rows_of_no_page_between_others(page, Hq, Hkv):
+    """Every third entry of the table is no page: its rows take no part, in blocks and row by row."""
+    B = mk()
+    capacity = page * (-(-200 // page))
+    c = C.make("bf16", [200, 0, 97], Hq, Hkv, 64, capacity, page, append=False, weights=True, seed=page)
+    bad = c["table_dev"].clone()
+    pages = bad.shape[1]
+    gone_pages = [i for i in range(pages) if i % 3 == 1]
+    bad[:, gone_pages] = torch.tensor([-1, c["k"].shape[0], -2 ** 31] * len(gone_pages), dtype=torch.int32, device="cuda")[:len(gone_pages)]
+    weight = c["weight"].clone()
+    res = B.metok_decode_attention_paged(c["q"], c["k"], c["v"], bad, c["lens_dev"], weight=c["weight"])
+    torch.cuda.synchronize()
+    left = [[j for j in range(len(x)) if (j // page) % 3 != 1] for x in c["rows64"][0]]
+    for b, x in enumerate(c["rows64"][0]):
+        for j in set(range(len(x))) - set(left[b]):
+            assert c["weight"][b, j] == weight[b, j]
+        if left[b]:
+            grown = (c["weight"][b] - weight[b]).double().sum().item()
+            assert abs(grown - 1) < 4 * 2.0 ** -24 * 2 * len(x) * float(weight.abs().max() + 1)       # the sums' and the differences' roundings
+    c["rows64"] = [[x[left[b]] for b, x in enumerate(c["rows64"][w])] for w in range(2)]
+    C.check(dict(c, weight=None), res)
