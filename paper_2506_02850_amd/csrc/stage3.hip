@@ -113,8 +113,8 @@ __device__ __forceinline__ int wave_lower_bound(const int32_t* __restrict__ idx,
     return lo;
 }
 
-// LISTED: the tiles of args.moved alone, in the same order.  A workgroup takes one ticket after the other, and while a ticket is on its way the tiles
-// before each (layer, video) are counted; a ticket behind the last tile ends it.  With a turn for every tile of the cache the tiles of videos
+// LISTED: the tiles of args.moved alone, in the same order.  A workgroup takes one ticket after the other and counts the tiles before each (layer,
+// video) once, into LDS; a ticket behind the last tile ends it.  With a turn for every tile of the cache the tiles of videos
 // that stay as they are, three quarters of them, each held a place on a CU to find that out (2 of 8 videos beyond the budget: 260 us).
 // A tile waits only for tiles of earlier tickets, whose workgroups hold no later one: the waits end as above.
 template <int MODE, bool LISTED = false>
@@ -127,6 +127,9 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
     // each, the others leave before they touch the counter.
     const int64_t n_items = MODE == kMoveRelink ? static_cast<int64_t>(*args.n_work) * n_sub : args.total_items;
     if (MODE == kMoveRelink && static_cast<int64_t>(blockIdx.x) >= n_items) return;
+    // LISTED: kMoveThreads groups at a time, how many tiles move before each; a workgroup's tickets ascend, so it never looks back
+    __shared__ int s_before[LISTED ? kMoveThreads + 1 : 1], s_first[LISTED ? kMoveThreads : 1];
+    int chunk = -kMoveThreads, counted = 0;
     for (bool more = true; more; more = LISTED) {
     if (threadIdx.x == 0) {
         const int g = blockIdx.x & (args.n_tickets - 1);
@@ -135,18 +138,25 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows_kernel(const MoveArgs 
     int slot = 0, b, tile, sub;
     if constexpr (LISTED) {
         __shared__ int s_scan[17], s_group, s_tile;
-        if (threadIdx.x == 0) s_group = -1;
         const int n_groups = args.n_layers * args.B;
-        for (int base = 0, done = 0; base < n_groups; base += kMoveThreads) {
-            const int g = base + static_cast<int>(threadIdx.x), of = g / args.B;
+        __syncthreads();
+        const int want = s_item / n_sub;
+        while (chunk < 0 || want >= counted) {
+            chunk += kMoveThreads;
+            if (chunk >= n_groups) return;
+            const int g = chunk + static_cast<int>(threadIdx.x), of = g / args.B;
             const int2 m = g < n_groups ? args.moved[static_cast<int64_t>(args.layer[of].layer_id) * args.B + (g - of * args.B)] : make_int2(0, 0);
             int here = 0;
-            const int before = done + block_exclusive_scan(m.y, s_scan, &here), want = s_item / n_sub;
-            if (want >= before && want < before + m.y) { s_group = g; s_tile = m.x + want - before; }
-            done += here;
+            const int before = counted + block_exclusive_scan(m.y, s_scan, &here);
+            counted += here;
+            s_before[threadIdx.x] = before;
+            s_first[threadIdx.x] = m.x;
+            if (threadIdx.x == 0) s_before[kMoveThreads] = counted;
+            __syncthreads();
         }
+        const int before = s_before[threadIdx.x];
+        if (want >= before && want < s_before[threadIdx.x + 1]) { s_group = chunk + static_cast<int>(threadIdx.x); s_tile = s_first[threadIdx.x] + want - before; }
         __syncthreads();
-        if (s_group < 0) return;
         slot = s_group / args.B;
         b = s_group - slot * args.B;
         tile = s_tile;
