@@ -303,3 +303,37 @@ def test_lengths_in_place_of_many_videos(S):
     res = B.metok_kv_evict_select([torch.from_numpy(x).cuda() for x in w], held, S, budget, 3, 11, new_len=held)
     torch.cuda.synchronize()
     check_selection(res, w, lists, new)
+
+
+@pytest.mark.parametrize("page", [0, 4])
+def test_caches_of_many_videos(page):
+    """More (layer, video) pairs than a workgroup of the row mover has threads; every third video is within the budget, some are empty."""
+    B = mk()
+    L, videos, Hkv, dh, S = 2, 1500, 2, 8, 40
+    rng = np.random.default_rng(page)
+    lens = rng.integers(21, S + 1, (L, videos)).astype(np.int32)
+    lens[:, ::3] = rng.integers(0, 21, lens[:, ::3].shape)
+    lens[:, 1000:1400] = 20                          # a long run in which nothing moves
+    w = [weights_of("attention", rng, (videos, S)) for _ in range(L)]
+    lists, new = expected(w, lens, [20] * L, 1, 3, S)
+    per_seq = S // page if page else 0
+    table = rng.permutation(videos * per_seq).reshape(videos, per_seq).astype(np.int32) if page else None
+    shape = (videos * per_seq, Hkv, page, dh) if page else (videos, Hkv, S, dh)
+    k, v = caches(rng, L, shape, "f32")
+    before = [[bits(t) for t in x] for x in (k, v)]
+    args = ([torch.from_numpy(x).cuda() for x in w], torch.from_numpy(lens).cuda(), 20, 1, 3)
+    res = B.metok_kv_evict_paged(k, v, torch.from_numpy(table).cuda(), *args) if page else B.metok_kv_evict(k, v, *args)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(res["new_len"].cpu().numpy(), new)
+    for l in range(L):
+        np.testing.assert_array_equal(res["idx"][l].cpu().numpy(), lists[l])
+        for old, now in ((before[0][l], bits(k[l])), (before[1][l], bits(v[l]))):
+            want = old.copy()
+            for b in range(videos):
+                n = new[l, b]
+                i, j = np.arange(n), lists[l][b, :n]
+                if page:
+                    want[table[b, i // page], :, i % page] = old[table[b, j // page], :, j % page]
+                else:
+                    want[b][:, i] = old[b][:, j]
+            np.testing.assert_array_equal(now, want)
