@@ -15,7 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmetok.so")
 HOST = os.path.join(HERE, "_host" + sysconfig.get_config_var("EXT_SUFFIX"))
-SOURCES = ["core.hip", "stage1.hip", "stage2.hip", "stage3.hip", "decode.hip", "decode_wide.hip", "evict.hip"]
+SOURCES = ["core.hip", "stage1.hip", "stage2.hip", "stage3.hip", "decode.hip", "decode_short.hip", "decode_wide.hip", "evict.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument"]

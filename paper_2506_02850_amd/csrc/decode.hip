@@ -153,6 +153,10 @@ static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) 
     const int64_t bytes = static_cast<int64_t>(a.B) * a.Hkv * a.S_cap * DH * static_cast<int64_t>(sizeof(T)) * 2;
     const unsigned groups = static_cast<unsigned>(plan.grid);
     const bool stream = bytes > kStreamBytes;
+    if (plan.whole) {
+        launch_short_attention(a, sizeof(T) == 2 ? METOK_BF16 : METOK_F32, DH, static_cast<unsigned>(plan.pairs), st);
+        return check_launch("decode attention");
+    }
     if (plan.wide) launch_wide_attention(a, sizeof(T) == 2 ? METOK_BF16 : METOK_F32, DH, groups, st);
     else if (!a.table) stream ? launch_attention<T, DH, kDense, true, 1>(a, groups, st) : launch_attention<T, DH, kDense, false, 1>(a, groups, st);
     else if (a.page_size % 16 != 0) launch_attention<T, DH, kRows, false, 1>(a, groups, st);

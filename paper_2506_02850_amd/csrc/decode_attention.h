@@ -160,34 +160,48 @@ enum { kDense = 0, kBlocks = 1, kRows = 2 };              // the cache; pages of
 // out equal, 131072 rows of 28 / 4 heads 46.7 us, 20 to 40 % slower where a third of the CUs had one more.)  K of the next tile is on
 // its way as soon as the scores are taken, V as soon as the sums are, across the end of a pair too; no load is conditional but
 // those of a new pair's queries and of the new row, so that the waits count the others exactly.
-template <typename T, int DH, int FORM, bool WEIGHTS, bool STREAM, int NB>
-__global__ __launch_bounds__(kAttendThreads, NB == 1 ? 2 : 1) void decode_attention_kernel(const DecodeArgs a) {
+//
+// WHOLE: a workgroup has a pair to itself, its waves the pair's tiles, neighbouring ones each, and joins their results in LDS.
+template <typename T, int DH, int FORM, bool WEIGHTS, bool STREAM, int NB, bool WHOLE = false>
+__global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB == 1 ? 2 : 1) void decode_attention_kernel(const DecodeArgs a) {
+    static_assert(!WHOLE || (NB == 1 && !WEIGHTS), "a pair is all query heads of a kv head");
     using S = AttendShape<T, DH>;
     constexpr bool BF16 = sizeof(T) == 2;
     constexpr int TILE = S::kTile, NT = S::kSub, KS = S::kPieces, NV = S::kKeys, E = S::kElems, VW = S::kWords, RB = S::kRowBytes;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
     // neighbouring workers on different CUs, so that few tiles are spread over all of them
     const int worker = wave * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
-    const Place place = find_place<TILE, Deal<attend_groups(sizeof(T), DH)>>(a, worker);
-    if (place.left <= 0) return;
     const bool fresh = a.k_new != nullptr;
     const scalar_ints lens = reinterpret_cast<scalar_ints>(reinterpret_cast<uintptr_t>(a.len));
 
     // A tile of a pair, its kv head and block of query heads: uniform over the wave.
     struct Cursor { int b, kvh, rb, t, tiles, n; };
     Cursor at;
-    at.b = __builtin_amdgcn_readfirstlane(place.b);
-    at.tiles = __builtin_amdgcn_readfirstlane(place.tiles);
-    at.n = __builtin_amdgcn_readfirstlane(place.n);
-    const int units = at.tiles + kAttendPairCost;
-    const int hr = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(place.at) / static_cast<uint32_t>(units)));
-    at.kvh = a.row_blocks == 1 ? hr : __builtin_amdgcn_readfirstlane(hr / a.row_blocks);
-    at.rb = hr - at.kvh * a.row_blocks;
-    at.t = __builtin_amdgcn_readfirstlane(place.at) - hr * units;
-    int left = __builtin_amdgcn_readfirstlane(place.left);
-    int n_ahead = lens[min(at.b + 1, a.B - 1)];
+    int left;                                              // units that the worker still has (WHOLE: tiles)
+    if constexpr (WHOLE) {
+        at.b = static_cast<int>(blockIdx.x) / a.Hkv;
+        at.kvh = static_cast<int>(blockIdx.x) - at.b * a.Hkv;
+        at.rb = 0;
+        at.n = min(max(lens[at.b], 0), a.S_cap);
+        at.tiles = max(static_cast<int>(static_cast<uint32_t>(at.n + static_cast<int>(fresh) + TILE - 1) / TILE), 1);
+        at.t = wave * at.tiles / kAttendWholeWaves;
+        left = (wave + 1) * at.tiles / kAttendWholeWaves - at.t;
+    } else {
+        const Place place = find_place<TILE, Deal<attend_groups(sizeof(T), DH)>>(a, worker);
+        if (place.left <= 0) return;
+        at.b = __builtin_amdgcn_readfirstlane(place.b);
+        at.tiles = __builtin_amdgcn_readfirstlane(place.tiles);
+        at.n = __builtin_amdgcn_readfirstlane(place.n);
+        const int units = at.tiles + kAttendPairCost;
+        const int hr = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(place.at) / static_cast<uint32_t>(units)));
+        at.kvh = a.row_blocks == 1 ? hr : __builtin_amdgcn_readfirstlane(hr / a.row_blocks);
+        at.rb = hr - at.kvh * a.row_blocks;
+        at.t = __builtin_amdgcn_readfirstlane(place.at) - hr * units;
+        left = __builtin_amdgcn_readfirstlane(place.left);
+    }
+    int n_ahead = WHOLE ? 0 : lens[min(at.b + 1, a.B - 1)];
     auto advance = [&](Cursor x) {
-        if (++x.t == x.tiles) {
+        if (++x.t == x.tiles && !WHOLE) {
             x.t = 0;
             if (++x.rb == a.row_blocks) {
                 x.rb = 0;
@@ -491,22 +505,23 @@ __global__ __launch_bounds__(kAttendThreads, NB == 1 ? 2 : 1) void decode_attent
         }
     };
 
-    if (at.t >= at.tiles) {                                // behind a pair: on to the next one, if there is one
+    if (!WHOLE && at.t >= at.tiles) {                                // behind a pair: on to the next one, if there is one
         left -= at.tiles + kAttendPairCost - at.t;
         if (left <= 0) return;
         at.t = at.tiles - 1;
         at = advance(at);
     }
+    clear();
+    if (!WHOLE || left > 0) {
     int begun = at.t;                                      // first tile of the pair that the worker has
     load_q(at, qf);
     Rows rows = rows_of(at, pages_of(at));
     load_k(at, rows);
     load_v(at, rows);
-    clear();
     // one block: the queries of the next pair are on their way with its first tile; several: the registers are needed
     u32x4_t q_next[NB == 1 ? NB : 1][KS];
     for (;;) {
-        const bool ends = at.t == at.tiles - 1;
+        const bool ends = !WHOLE && at.t == at.tiles - 1;
         left -= ends ? 1 + kAttendPairCost : 1;
         if (left <= 0) break;
         const Cursor next = advance(at);
@@ -536,8 +551,46 @@ __global__ __launch_bounds__(kAttendThreads, NB == 1 ? 2 : 1) void decode_attent
     f32x4_t s[NB][NT];
     scores(s);
     take(at, rows, s);
-    finish(at, begun);
+    if constexpr (!WHOLE) finish(at, begun);
     append(at);
+    }
+    if constexpr (WHOLE) {
+        constexpr int W = kAttendWholeWaves, N = S::kRun, PITCH = DH + 4, LPR = DH / 4;       // 4 more: rows 16 bytes apart in the banks
+        __shared__ float4 s_o[W * kAttendRows * PITCH / 4];
+        __shared__ float2 s_ml[W][kAttendRows];
+        const float sum = swap32_add(swap16_add(l[0], l[0]), swap16_add(l[0], l[0]));
+        if (c == 0) s_ml[wave][r] = make_float2(m[0], sum);
+        float* to = reinterpret_cast<float*>(s_o) + (wave * kAttendRows + r) * PITCH;
+#pragma unroll
+        for (int g = 0; g < S::kRuns; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < N; ++e) to[g * 16 * N + N * (4 * c + i) + e] = acc[0][g * N + e][i];
+        __syncthreads();
+        const int x = threadIdx.x % LPR, heads = n_heads(at);
+        for (int row = threadIdx.x / LPR; row < heads; row += 64 * W / LPR) {
+            float top = -INFINITY, total = 0.f;
+#pragma unroll
+            for (int w = 0; w < W; ++w) top = fmaxf(top, s_ml[w][row].x);
+            const float ref = top == -INFINITY ? 0.f : top;
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float2 part = s_ml[w][row];
+                const float f = exp2_of(part.x - ref);
+                const float4 v = s_o[((w * kAttendRows + row) * PITCH + 4 * x) / 4];
+                total = fmaf(part.y, f, total);
+                o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+            }
+            const float inv = total == 0.f ? 0.f : 1.f / total;
+            const int64_t head = static_cast<int64_t>(at.b) * a.Hq + first_head(at) + row;
+            char* out = a.out + head * RB + 4 * x * static_cast<int>(sizeof(T));
+            if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+            else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+            if (x == 0 && a.lse) a.lse[head] = total == 0.f ? -INFINITY : (ref + log2_of(total)) * 0.693147180559945309f;
+        }
+    }
 }
 
 template <typename T, int DH, int FORM, bool STREAM, int NB>
@@ -547,5 +600,7 @@ void launch_attention(const DecodeArgs& a, unsigned groups, hipStream_t st) {
 }
 // The same with several blocks of query heads to a kv head at a time (decode_wide.hip).
 void launch_wide_attention(const DecodeArgs& a, int dtype, int dh, unsigned groups, hipStream_t st);
+// Short caches, a workgroup to a pair, in one launch (decode_short.hip).
+void launch_short_attention(const DecodeArgs& a, int dtype, int dh, unsigned pairs, hipStream_t st);
 
 }  // namespace metok

@@ -16,6 +16,13 @@ constexpr int attend_tile(int esize, int dh) { return esize * dh <= 256 && esize
 // four; of 2 heads of 64: 58, 62).
 constexpr int attend_groups(int esize, int dh) { return 2 * attend_tile(esize, dh) * esize * dh <= 4096 ? 512 : 256; }
 
+// Capacities of up to so many tiles (no weights, at most 16 query heads to a kv head) take a workgroup of eight waves per pair and no second
+// launch.  With more tiles than that few pairs leave most of the chip idle.  One video, 28 heads on 4 of 128: 128 rows 4.4 us (8.9 split over
+// all CUs and joined), 512 rows 7.8 (8.9), 1024 rows, 33 tiles, 12.3 (9.0); 64 of them 6.0 (12.4), 13.0 (19.4), 27.6 (33.9), 256 17.4 (22.1),
+// 51.4 (50.6), 96 (87); 2 videos of 14 heads on 2 of 64 in fp32, tiles of 16 rows: 256 rows 6.0 (8.4); 2 of 8 on 2 of 256: 512 rows, 33
+// tiles, 12.7 (8.8).
+constexpr int kAttendWholeWaves = 8, kAttendWhole = 32;
+
 // The tiles of all (video, kv head, row block) pairs, one pair behind the other, are dealt out evenly to the waves, the workers.  The end of a
 // pair takes a worker about as long as a tile, so every pair counts kAttendPairCost tiles more than it has; they lie behind its own (32 videos of 0
 // to 8191 rows, 32 heads on 8: 41 us without, 32 with one, 31.5 with two; many short pairs fell to few workers).
@@ -44,6 +51,7 @@ struct AttendPlan {
     int64_t pairs;         // (video, kv head, row block): what is split over the rows of the cache
     int64_t grid;          // workgroups
     int64_t workers;       // at most
+    bool whole;            // a workgroup to a pair, no second launch and no workspace
     bool joined;           // false: every pair is one tile, whatever the lengths
     int64_t logit_stride;  // logits of a (video, query head), 0: not kept
     size_t pair_workers, part_ml, part_o, lse2, logits, bytes;       // offsets in the workspace, and its size
@@ -60,7 +68,8 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     p.rows = group < p.block_rows ? group : p.block_rows;
     p.pairs = static_cast<int64_t>(B) * Hkv * p.row_blocks;
     const int64_t most = (capacity + 1 + p.tile - 1) / p.tile;                       // tiles of the longest video
-    p.joined = most > 1;
+    p.whole = !p.wide && !with_weight && most <= kAttendWhole;
+    p.joined = most > 1 && !p.whole;
     const int groups = attend_groups(esize, dh);
     const int64_t few = ((most + kAttendPairCost) * p.pairs + kAttendMinTiles - 1) / kAttendMinTiles;      // workers, with a workgroup each
     p.grid = few < groups ? few : groups;

@@ -142,7 +142,7 @@ using namespace metok;
 extern "C" void attend_plan(int B, int Hq, int Hkv, int64_t cap, int dh, int esize, int w, int64_t* o) {
     const AttendPlan p = plan_attend(B, Hq, Hkv, cap, dh, esize, w != 0);
     for (int64_t v : {int64_t(p.tile), int64_t(p.row_blocks), int64_t(p.block_rows), int64_t(p.rows), p.pairs, p.grid, p.workers, int64_t(p.joined), p.logit_stride, int64_t(p.pair_workers),
-                      int64_t(p.part_ml), int64_t(p.part_o), int64_t(p.lse2), int64_t(p.logits), int64_t(p.bytes), int64_t(attend_groups(esize, dh))}) *o++ = v;
+                      int64_t(p.part_ml), int64_t(p.part_o), int64_t(p.lse2), int64_t(p.logits), int64_t(p.bytes), int64_t(attend_groups(esize, dh)), int64_t(p.whole)}) *o++ = v;
 }
 extern "C" int64_t workers(int groups, int64_t units) { return groups == 512 ? Deal<512>::workers(units) : Deal<256>::workers(units); }
 extern "C" int64_t first(int groups, int64_t w, int64_t units) { return groups == 512 ? Deal<512>::first(w, units) : Deal<256>::first(w, units); }
@@ -186,10 +186,14 @@ def test_partial_results_have_slots_of_their_own(seed):
         esize, dh = rng.choice([(2, 128), (4, 64), (2, 256), (2, 32), (4, 32)])
         cap = int(2 ** rng.uniform(0, 13))
         w = rng.randint(0, 1)
-        o = (ctypes.c_int64 * 16)()
+        o = (ctypes.c_int64 * 17)()
         lib.attend_plan(Bn, Hq, Hkv, ctypes.c_int64(cap), dh, esize, w, o)
-        tile, row_blocks, block_rows, rows, pairs, grid, most_workers, joined, stride, table, ml, part, lse2, logits, total, groups = list(o)
+        tile, row_blocks, block_rows, rows, pairs, grid, most_workers, joined, stride, table, ml, part, lse2, logits, total, groups, whole = list(o)
         heads = Hkv * row_blocks
+        if whole:                                                        # a workgroup to a pair: nothing is left for another one
+            assert not w and Hq // Hkv <= 16 and total == 0 and not joined
+            assert -(-(cap + 1) // tile) <= 32 and pairs == Bn * Hkv
+            continue
         assert pairs == Bn * heads and block_rows * row_blocks >= Hq // Hkv > (row_blocks - 1) * block_rows and rows == min(block_rows, Hq // Hkv) and most_workers == 4 * groups
         slots = (part - ml) // (rows * 2 * 4)
         for kind in range(4):

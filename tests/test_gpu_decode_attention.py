@@ -331,3 +331,39 @@ def test_rows_of_no_page_between_others(page, Hq, Hkv):
             assert abs(grown - 1) < 4 * 2.0 ** -24 * 2 * len(x) * float(weight.abs().max() + 1)       # the sums' and the differences' roundings
     c["rows64"] = [[x[left[b]] for b, x in enumerate(c["rows64"][w])] for w in range(2)]
     C.check(dict(c, weight=None), res)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 32), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [0, 16, 7])
+def test_every_kernel_of_long_capacities(dtype, dh, page):
+    """Caches that could be long are split over all workgroups even while they are short."""
+    lens = [0, 1, 15, 16, 17, 31, 32, 33, 129, 300]
+    capacity = 1100 if page == 0 else page * (-(-1100 // page))
+    Hq, Hkv = [(28, 4), (4, 4), (14, 2), (16, 1), (8, 2), (32, 8), (1, 1)][(dh // 32 + page) % 7]
+    run(C.make(dtype, lens, Hq, Hkv, dh, capacity, page, append=True, seed=dh + page))
+    run(C.make(dtype, lens, Hq, Hkv, dh, capacity, page, append=False, cap=20.0, seed=dh + page + 1))
+
+
+@pytest.mark.parametrize("capacity", [31, 32, 255, 256, 510, 511, 512, 1022, 1023, 1024])
+@pytest.mark.parametrize("dtype,dh", [("bf16", 128), ("f32", 64), ("bf16", 256)])
+def test_capacities_where_the_form_changes(capacity, dtype, dh):
+    """On both sides of the number of tiles that one workgroup takes, full caches and nearly full ones."""
+    run(C.make(dtype, [capacity, capacity - 1, capacity // 2, 0], 8, 2, dh, capacity, append=True, seed=capacity))
+    run(C.make(dtype, [capacity, 1], 16, 1, dh, capacity, append=False, cap=5.0, seed=capacity + 1))
+
+
+def test_short_caches_need_no_workspace():
+    B = mk()
+    c = C.make("bf16", [100, 0, 511], 28, 4, 128, 511, 7, append=True, seed=2)
+    assert B.metok_decode_attention_workspace_bytes(3, 28, 4, 511, 128, B.BF16) == 0
+    first = C.call(B, c)
+    torch.cuda.synchronize()
+    C.check(c, first)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        C.call(B, c, out=first)
+    for _ in range(3):
+        first["out"].fill_(7.0)
+        g.replay()
+        torch.cuda.synchronize()
+        C.check(c, first)
