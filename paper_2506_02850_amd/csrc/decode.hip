@@ -1,13 +1,15 @@
 // Attention of one new token per video over the dense or paged KV cache that stage 3 leaves (Sec. 3.3), with the token's own row
 // appended and, if asked, the attention weight of every cached row accumulated (what metok_kv_evict ranks the rows by).
 //
-//   decode_attention_kernel  every wave's tiles of the rows of all (video, kv head, block of 16 query heads): scores, running maximum and
-//                            sum of the softmax, weighted sum of the values, in one pass over K and V
+//   decode_attention_kernel  (decode_attention.h) every wave's tiles of the rows of all (video, kv head, block of query heads): scores,
+//                            running maximum and sum of the softmax, weighted sum of the values, in one pass over K and V
 //   decode_join_kernel       joins the parts of a (video, query head) whose rows several waves had; and, with weights, turns the
 //                            scores that the first kernel kept into probabilities and adds their mean over the heads to the rows' weights
 //
 // What bounds it is the stream of K and V: 4 Hq dh operations a row on 2 Hkv dh elements, 7 operations a byte with seven query
 // heads to a kv head in bf16.  The query heads of a kv head are the columns of one MFMA, so a row is read once for all of them.
+// 8 videos of 36992 rows, 28 heads on 4 of 128 in bf16, 606 MB: 95.5 us a call, 6.35 TB/s (the join 4.5 us of it; a copy of 1 GiB moves
+// 6.65 TB/s).  One of 2306 rows 8.6 us: two launches and their latency.
 #include "decode_attention.h"
 
 namespace metok {
