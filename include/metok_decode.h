@@ -92,6 +92,7 @@ METOK_API int metok_decode_attention_paged(const void* q, int B, int Hq, int Hkv
  *   reads or writes; of idx, weight, weight_out, len and new_len that is checked.
  * metok_kv_evict and metok_kv_evict_paged select and move the rows of the caches (row i <- row idx[l][b][i]; rows from
  * new_len on are left as they were); metok_kv_evict_select only selects, for callers that relink pages or move the rows themselves.
+ *   Paged: rows are moved in place, so pages that videos share may only hold rows that no video moves: among their first n_first ones.
  *   workspace    metok_kv_evict_workspace_bytes() for the first two, none for the selection; as in metok_kv_compact its first word
  *                is 0 after the call unless a bounded wait expired.
  * ------------------------------------------------------------------------------------------- */

@@ -8,7 +8,7 @@
 // sixteenth of the rows, 64 neighbouring rows an instruction, so that the place of a kept row is a population count of lane
 // masks away from the number of rows that earlier waves keep: one exchange between the waves, no scan per tile.
 // What bounds it is latency: a video of 4224 rows is 17 KB, and some ten barriers and round trips to LDS come one behind the other.  Kernel
-// times: 28 x 1 of 4224 rows 8.8 us, 28 x 8 of up to 4096 rows 9.1, 28 x 4 of 18560 rows 21.5, two of 100 rows 6.0.
+// times: 28 x 1 of 4224 rows 8.8 us, 28 x 8 of up to 4096 rows 9.1, 28 x 4 of 18560 rows 21.5, two of 777 rows 6.0.
 #include <algorithm>
 
 #include "common.h"

@@ -337,3 +337,26 @@ def test_caches_of_many_videos(page):
                 else:
                     want[b][:, i] = old[b][:, j]
             np.testing.assert_array_equal(now, want)
+
+
+def test_pages_shared_among_the_first_rows():
+    """Two videos share the pages of their first 32 rows, which stay: nothing there moves."""
+    B = mk()
+    rng = np.random.default_rng(4)
+    videos, Hkv, page, dh, S = 2, 2, 16, 32, 320
+    lens = np.array([[300, 277]], dtype=np.int32)
+    w = [weights_of("attention", rng, (videos, S))]
+    lists, new = expected(w, lens, [150], 32, 20, S)
+    table = rng.permutation(videos * 20).reshape(videos, 20).astype(np.int32)
+    table[1, :2] = table[0, :2]
+    k, v = caches(rng, 1, (videos * 20, Hkv, page, dh), "bf16")
+    before = [bits(k[0]), bits(v[0])]
+    res = B.metok_kv_evict_paged(k, v, torch.from_numpy(table).cuda(), [torch.from_numpy(w[0]).cuda()], torch.from_numpy(lens).cuda(), 150, 32, 20)
+    torch.cuda.synchronize()
+    check_selection(res, w, lists, new)
+    for old, now in zip(before, (bits(k[0]), bits(v[0]))):
+        want = old.copy()
+        for b in range(videos):
+            i, j = np.arange(150), lists[0][b]
+            want[table[b, i // page], :, i % page] = old[table[b, j // page], :, j % page]
+        np.testing.assert_array_equal(now, want)
