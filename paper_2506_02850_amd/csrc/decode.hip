@@ -147,7 +147,8 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
 }
 
 // Caches of more than this many bytes are read with the streaming hint: 375 MB (4 x 4571 rows, 40 heads of 128) 91 us without, 81 with; 606 MB
-// 109 and 98; a tenth of them, that the memory-side cache still holds from the call before, 16.5 and 18.1 (67 MB).
+// 109 and 98; a tenth of them, that the memory-side cache still holds from the call before, 16.5 and 18.1 (67 MB).  Row by row (8 x 36990 rows in pages of 7 / 8 / 1)
+// 116 / 112 / 123 without, 112 / 110 / 124 with.
 constexpr int64_t kStreamBytes = 128 << 20;
 
 template <typename T, int DH>
@@ -161,7 +162,7 @@ static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) 
     }
     if (plan.wide) launch_wide_attention(a, sizeof(T) == 2 ? METOK_BF16 : METOK_F32, DH, groups, st);
     else if (!a.table) stream ? launch_attention<T, DH, kDense, true, 1>(a, groups, st) : launch_attention<T, DH, kDense, false, 1>(a, groups, st);
-    else if (a.page_size % 16 != 0) launch_attention<T, DH, kRows, false, 1>(a, groups, st);
+    else if (a.page_size % 16 != 0) stream ? launch_attention<T, DH, kRows, true, 1>(a, groups, st) : launch_attention<T, DH, kRows, false, 1>(a, groups, st);
     else stream ? launch_attention<T, DH, kBlocks, true, 1>(a, groups, st) : launch_attention<T, DH, kBlocks, false, 1>(a, groups, st);
     int rc = check_launch("decode attention");
     if (rc) return rc;

@@ -367,3 +367,14 @@ def test_short_caches_need_no_workspace():
         g.replay()
         torch.cuda.synchronize()
         C.check(c, first)
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 32), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [0, 16, 7])
+def test_every_kernel_of_large_caches(dtype, dh, page):
+    """Caches beyond the 128 MB from which on they are read past the caches of the chip, with few rows in them, and many in one."""
+    row = 2 * 2 * dh * (2 if dtype == "bf16" else 4)
+    unit = page or 1
+    capacity = ((140 << 20) // (row * 4) // unit + 1) * unit
+    run(C.make(dtype, [0, 33, 1500, 100], 8, 2, dh, capacity, page, append=True, seed=dh + page))
+    run(C.make(dtype, [0, 33, 1500, 100], 8, 2, dh, capacity, page, append=page == 0, weights=True, seed=dh + page + 1))
