@@ -160,7 +160,7 @@ static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) 
         launch_short_attention(a, sizeof(T) == 2 ? METOK_BF16 : METOK_F32, DH, static_cast<unsigned>(plan.pairs), st);
         return check_launch("decode attention");
     }
-    if (plan.wide) launch_wide_attention(a, sizeof(T) == 2 ? METOK_BF16 : METOK_F32, DH, groups, st);
+    if (plan.wide) launch_wide_attention(a, sizeof(T) == 2 ? METOK_BF16 : METOK_F32, DH, stream, groups, st);
     else if (!a.table) stream ? launch_attention<T, DH, kDense, true, 1>(a, groups, st) : launch_attention<T, DH, kDense, false, 1>(a, groups, st);
     else if (a.page_size % 16 != 0) stream ? launch_attention<T, DH, kRows, true, 1>(a, groups, st) : launch_attention<T, DH, kRows, false, 1>(a, groups, st);
     else stream ? launch_attention<T, DH, kBlocks, true, 1>(a, groups, st) : launch_attention<T, DH, kBlocks, false, 1>(a, groups, st);

@@ -602,7 +602,7 @@ void launch_attention(const DecodeArgs& a, unsigned groups, hipStream_t st) {
     else hipLaunchKernelGGL((decode_attention_kernel<T, DH, FORM, false, STREAM, NB>), dim3(groups), dim3(kAttendThreads), 0, st, a);
 }
 // The same with several blocks of query heads to a kv head at a time (decode_wide.hip).
-void launch_wide_attention(const DecodeArgs& a, int dtype, int dh, unsigned groups, hipStream_t st);
+void launch_wide_attention(const DecodeArgs& a, int dtype, int dh, bool stream, unsigned groups, hipStream_t st);
 // Short caches, a workgroup to a pair, in one launch (decode_short.hip).
 void launch_short_attention(const DecodeArgs& a, int dtype, int dh, unsigned pairs, hipStream_t st);
 

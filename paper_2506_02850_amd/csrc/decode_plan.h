@@ -8,8 +8,9 @@ namespace metok {
 
 constexpr int kAttendWaves = 4, kAttendThreads = 64 * kAttendWaves;
 constexpr int kAttendRows = 16;                // query rows of a block: one MFMA's columns
-// Blocks of a wave where a kv head has more than one: what fits the registers beside K, V and the sums.
-constexpr int attend_blocks(int dh) { return dh <= 64 ? 4 : 2; }
+// Blocks of a wave where a kv head has more than one: four where they fit the registers beside K, V and the sums and more than two are there
+// (8 x 149990 rows of 64 elements, 24 query heads on one kv head: 82 us with four, 62 with two; 48 of them 81 and 93; 71 of them 141 and 159).
+constexpr int attend_blocks(int dh, int group) { return dh <= 64 && group > 2 * kAttendRows ? 4 : 2; }
 // Cache rows of a tile: K and V of the next one are on their way in registers, 64 of them at most.
 constexpr int attend_tile(int esize, int dh) { return esize * dh <= 256 && esize == 2 ? 32 : 16; }
 // Workgroups of a large call: one per CU, two where a tile is only 4 KB (8 x 73980 rows of 4 heads of 32 bf16: 68 us with one, 57 with two, 57 with
@@ -63,7 +64,7 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     const int group = Hq / Hkv;
     p.tile = attend_tile(esize, dh);
     p.wide = group > kAttendRows;
-    p.block_rows = kAttendRows * (p.wide ? attend_blocks(dh) : 1);
+    p.block_rows = kAttendRows * (p.wide ? attend_blocks(dh, group) : 1);
     p.row_blocks = (group + p.block_rows - 1) / p.block_rows;
     p.rows = group < p.block_rows ? group : p.block_rows;
     p.pairs = static_cast<int64_t>(B) * Hkv * p.row_blocks;

@@ -378,3 +378,15 @@ def test_every_kernel_of_large_caches(dtype, dh, page):
     capacity = ((140 << 20) // (row * 4) // unit + 1) * unit
     run(C.make(dtype, [0, 33, 1500, 100], 8, 2, dh, capacity, page, append=True, seed=dh + page))
     run(C.make(dtype, [0, 33, 1500, 100], 8, 2, dh, capacity, page, append=page == 0, weights=True, seed=dh + page + 1))
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 32), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [0, 16, 7])
+@pytest.mark.parametrize("Hq", [24, 64])
+def test_every_kernel_of_many_query_heads_and_large_caches(dtype, dh, page, Hq):
+    """The same beyond 128 MB, with two blocks of query heads at a time and, where they fit, four; and caches below that."""
+    row = 2 * dh * (2 if dtype == "bf16" else 4)
+    unit = page or 1
+    capacity = ((140 << 20) // (row * 3) // unit + 1) * unit
+    run(C.make(dtype, [0, 700, 45], Hq, 1, dh, capacity, page, append=True, weights=Hq == 24, seed=dh + page))
+    run(C.make(dtype, [0, 700, 45], Hq, 1, dh, 200 * max(unit, 4), page, append=False, cap=10.0, weights=Hq == 64, seed=dh + page + 1))
