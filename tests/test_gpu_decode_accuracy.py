@@ -1,0 +1,40 @@
+"""GPU tests of how exact metok_decode_attention is, with bounds near its own roundings (those of decode_cases.py are worst cases)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24                                   # half a step of fp32
+TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
+# One launch (200 rows without weights) and split over the chip; some shares of a wave are a part, some a whole video.
+FORMS = [(200, False), (200, True), (40, True), (3000, False), (3000, True), (20000, False)]
+
+
+def mk():
+    from paper_2506_02850_amd import binding as B
+    return B
+
+
+def around(offset, rows, dtype, seed, videos=4, heads=4, kv_heads=2, dh=64):
+    """q and K whose scores lie around `offset`, with a standard deviation of about 1; all numbers fit both types."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    k = torch.randn((videos, kv_heads, rows, dh), generator=g, device="cuda")
+    q = torch.randn((videos, heads, dh), generator=g, device="cuda")
+    q[..., 0], k[..., 0] = 16.0, offset / 16.0 * dh ** 0.5
+    return q.to(TORCH[dtype]), k.to(TORCH[dtype])
+
+
+@pytest.mark.parametrize("rows,weights", FORMS)
+@pytest.mark.parametrize("offset", [0.0, 60.0, 200.0, 700.0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_equal_values_come_out_as_they_are(rows, weights, offset, dtype):
+    """All rows of V are 1: the result is the sum of the probabilities, 1 whatever the scores.  Output and sum add up the same fp32 numbers
+    in other orders, some 240 additions in a chain at most, each off by u of the sum so far: 3 sqrt(240 / 3) u = 27 u at three
+    standard deviations, 32 u with the division and the factors between the parts.  bf16: a probability in two parts is 2^-17 off at
+    most, which rounds to 1."""
+    q, k = around(offset, rows, dtype, seed=rows)
+    v = torch.ones_like(k)
+    lens = torch.tensor([rows, rows - 1, rows // 2, 1], dtype=torch.int32, device="cuda")
+    res = mk().metok_decode_attention(q, k, v, lens, weight=torch.zeros((4, rows), device="cuda") if weights else None)
+    far = (res["out"].double() - 1).abs().max().item()
+    assert far <= (32 * U if dtype == "f32" else 0.0), f"{far / U:.1f} u"
