@@ -27,8 +27,8 @@ struct DecodeArgs {
     int2* pair_workers;          // [pairs]: first and last worker of a (video, kv head, row block)
     float* part_ml;              // [slots][rows][2]: maximum and sum of a partial result, log2 domain
     float* part_o;               // [slots][rows][dh]
-    float* lse2;                 // [B, Hq]: log2 of the sum, where one worker had all rows
-    float* logits;               // [B, Hq, logit_stride], log2 domain
+    float2* norm;                // [B, Hq]: maximum (log2 domain) and 1 / sum, 0 and 0 without rows, where one worker had all of them
+    float* logits;               // [B, Hq, logit_stride]: without cap before the scale, with cap in the log2 domain
     int64_t weight_stride, logit_stride;
     int B, Hq, Hkv, group, row_blocks, block_rows, rows;
     int S_cap;                   // capacity
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
                 if (16 * nb + r < n_heads(x)) {
                     float* to = a.logits + (static_cast<int64_t>(x.b) * a.Hq + first_head(x) + 16 * nb + r) * a.logit_stride + x.t * TILE + 4 * c;
 #pragma unroll
-                    for (int b = 0; b < NT; ++b) *reinterpret_cast<f32x4_t*>(to + 16 * b) = s[nb][b] * scale;
+                    for (int b = 0; b < NT; ++b) *reinterpret_cast<f32x4_t*>(to + 16 * b) = s[nb][b];
                 }
         }
         float p[NB][NV];
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
                         }
                 }
                 if (c == 0 && r < heads && a.lse) a.lse[head] = lse2 * 0.693147180559945309f;
-                if (WEIGHTS && c == 0 && r < heads) a.lse2[head] = lse2;
+                if (WEIGHTS && c == 0 && r < heads) a.norm[head] = make_float2(sum == 0.f ? 0.f : m[nb], inv);
             } else {
                 if (r < heads) {
                     float* to = a.part_o + slot * DH;

@@ -56,6 +56,7 @@ struct AttendPlan {
     bool joined;           // false: every pair is one tile, whatever the lengths
     int64_t logit_stride;  // logits of a (video, query head), 0: not kept
     size_t pair_workers, part_ml, part_o, lse2, logits, bytes;       // offsets in the workspace, and its size
+                           // (lse2: a head's maximum and 1 / sum, what the logarithm of its sum is made of)
 };
 
 // `capacity` rows at most, one more with a new row.
@@ -88,7 +89,7 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     const size_t slots = p.joined ? static_cast<size_t>(2 * p.workers) * p.rows : 0;
     p.part_ml = take(slots * 2);
     p.part_o = take(slots * dh);
-    p.lse2 = take(with_weight ? static_cast<size_t>(B) * Hq : 0);
+    p.lse2 = take(with_weight ? static_cast<size_t>(B) * Hq * 2 : 0);
     p.logits = take(static_cast<size_t>(B) * Hq * static_cast<size_t>(p.logit_stride));
     p.bytes = at;
     return p;

@@ -38,3 +38,19 @@ def test_equal_values_come_out_as_they_are(rows, weights, offset, dtype):
     res = mk().metok_decode_attention(q, k, v, lens, weight=torch.zeros((4, rows), device="cuda") if weights else None)
     far = (res["out"].double() - 1).abs().max().item()
     assert far <= (32 * U if dtype == "f32" else 0.0), f"{far / U:.1f} u"
+
+
+@pytest.mark.parametrize("rows", [40, 200, 3000, 20000])
+@pytest.mark.parametrize("offset", [0.0, 60.0, 200.0, 700.0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_weights_of_a_step_add_up_to_one(rows, offset, dtype):
+    """One query head, weights that start at 0, added up in 64 bits: the probabilities' sum.  The sum that they were divided by has the chains of
+    the test above (27 u); the probabilities are computed once more for the weights, from the same scores: exponents up to 24 below
+    the largest, each rounded once (17 u there, and of random sign), an exp2 of 2 u.  40 u."""
+    videos = 6
+    q, k = around(offset, rows, dtype, seed=rows + 1, videos=videos, heads=1, kv_heads=1)
+    lens = torch.tensor([rows, rows - 1, rows // 2, 33, 16, 1], dtype=torch.int32, device="cuda")
+    w = torch.zeros((videos, rows), device="cuda")
+    mk().metok_decode_attention(q, k, torch.ones_like(k), lens, weight=w)
+    far = (w.double().sum(1) - 1).abs().max().item()
+    assert far <= 40 * U, f"{far / U:.1f} u"
