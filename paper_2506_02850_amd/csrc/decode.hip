@@ -19,10 +19,10 @@ constexpr int kWeightRows = kJoinThreads;       // cache rows a workgroup adds u
 // Up to so many workgroups a head's elements are spread over several of them, 32 each: with few heads every one has many parts (one
 // video of 2307 rows, 28 heads: 10.1 us a call with one workgroup a head, 9.0 with four).
 constexpr int kJoinSpread = 512;
-// (m, l) stands for the sum l 2^m.
-__device__ __forceinline__ void add_sum(float& m, float& l, float m2, float l2) {
+// (m, l) stands for the sum l 2^(m scale).
+__device__ __forceinline__ void add_sum(float& m, float& l, float m2, float l2, float scale) {
     const float to = fmaxf(m, m2), ref = to == -INFINITY ? 0.f : to;
-    l = l * exp2_of(m - ref) + l2 * exp2_of(m2 - ref);
+    l = l * exp2_from(m, ref, scale) + l2 * exp2_from(m2, ref, scale);
     m = to;
 }
 
@@ -41,6 +41,7 @@ template <typename T, int DH>
 __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml);
+    const float scale = score_scale(a);
     if (static_cast<int>(blockIdx.x) < a.join_blocks) {
         // One (video, query head), or 4 join_lanes of its elements.  Every wave sums up the parts' statistics for itself; the parts of the output
         // are on their way meanwhile, the first kAhead of every group of lanes.
@@ -65,22 +66,22 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
 #pragma unroll 4
         for (int p = lane; p < parts.n; p += 64) {
             const float2 v = ml[parts.slot(p)];
-            add_sum(m, l, v.x, v.y);
+            add_sum(m, l, v.x, v.y, scale);
         }
         const float top = score_of_key(wave_extreme<true>(ordered_key(m))), ref = top == -INFINITY ? 0.f : top;
         // The parts are added up relative to the largest maximum and divided by the sum, not scaled by 2^(m - log2 of the sum): that logarithm, rounded
         // at its full size, is off by a common factor of the result (fp32, 3000 rows with scores around 700: 1.9e-5 off, 1e-7 so).
-        l = wave_sum(l * exp2_of(m - ref));
+        l = wave_sum(l * exp2_from(m, ref, scale));
         const float inv = l == 0.f ? 0.f : 1.f / l;                           // 0: no row counts
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         auto add = [&](const float4& v, float f) { o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w); };
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            if (g + k * groups < parts.n) add(ahead[k], exp2_of(ahead_m[k] - ref));
+            if (g + k * groups < parts.n) add(ahead[k], exp2_from(ahead_m[k], ref, scale));
 #pragma unroll 4
         for (int p = g + kAhead * groups; p < parts.n; p += groups) {
             const int64_t slot = parts.slot(p);
-            add(*reinterpret_cast<const float4*>(part + slot * DH), exp2_of(ml[slot].x - ref));
+            add(*reinterpret_cast<const float4*>(part + slot * DH), exp2_from(ml[slot].x, ref, scale));
         }
         s_part[threadIdx.x] = o;
         __syncthreads();
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
         }
         if (threadIdx.x == 0 && piece == 0) {
             const int64_t at = static_cast<int64_t>(b) * a.Hq + head;
-            if (a.lse) a.lse[at] = (ref + log2_of(l)) * 0.693147180559945309f;       // log2(0) is -inf
+            if (a.lse) a.lse[at] = fmaf(ref, scale, log2_of(l)) * 0.693147180559945309f;       // log2(0) is -inf
         }
         return;
     }
@@ -107,8 +108,9 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
     const int w = static_cast<int>(blockIdx.x) - a.join_blocks, b = w / a.weight_blocks, first = w - b * a.weight_blocks;
     const int fresh = a.k_new != nullptr, n_cache = rows_before(a, b), n = min(n_cache + fresh, a.S_cap);       // rows that have a place
     if (static_cast<int64_t>(first) * kWeightRows >= n) return;
-    // Maximum and 1 / sum of every head (0 and 0 where no row counts): a.head_lanes neighbouring lanes to a head.  Apart, not as the rounded logarithm of
-    // the sum, and the scores unscaled, as the sums were taken of them: a step's weights add up to 1 (fp32, 20000 rows with scores around 700, one head: 2.7e-5 off through the logarithm, 9e-8 so).
+    // Maximum and 1 / sum of every head (0 and 0 where no row counts): a.head_lanes neighbouring lanes to a head.  Apart, not as the rounded logarithm
+    // of the sum, and the scores unscaled, as the sums were taken of them: a step's weights add up to 1 (fp32, 20000 rows with scores around
+    // 700, one head: 2.7e-5 off through the logarithm, 9e-8 so).
     for (int h0 = 0; h0 < a.Hq; h0 += kJoinThreads / a.head_lanes) {
         const int h = min(h0 + static_cast<int>(threadIdx.x) / a.head_lanes, a.Hq - 1), part = threadIdx.x % a.head_lanes;
         const HeadParts parts = parts_of(a, b, h);
@@ -116,14 +118,14 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
 #pragma unroll 8
         for (int p = part; p < (parts.n > 1 ? parts.n : 0); p += a.head_lanes) {
             const float2 v = ml[parts.slot(p)];
-            add_sum(m, l, v.x, v.y);
+            add_sum(m, l, v.x, v.y, scale);
         }
-        for (int off = a.head_lanes / 2; off; off >>= 1) add_sum(m, l, __shfl_xor(m, off, 64), __shfl_xor(l, off, 64));
+        for (int off = a.head_lanes / 2; off; off >>= 1) add_sum(m, l, __shfl_xor(m, off, 64), __shfl_xor(l, off, 64), scale);
         const float2 norm = parts.n == 1 ? a.norm[static_cast<int64_t>(b) * a.Hq + h] : l == 0.f ? make_float2(0.f, 0.f) : make_float2(m, 1.f / l);
         if (part == 0) s_norm[h] = norm;
     }
     __syncthreads();
-    const float inv = 1.f / static_cast<float>(a.Hq), scale = a.cap > 0.f ? 1.f : a.scale;
+    const float inv = 1.f / static_cast<float>(a.Hq);
     for (int64_t j0 = static_cast<int64_t>(first) * kWeightRows; j0 < n; j0 += static_cast<int64_t>(a.weight_blocks) * kWeightRows) {
         const int64_t j = j0 + 4 * lane;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -133,8 +135,8 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
             for (int h = wave; h < a.Hq; h += kJoinThreads / 64) {
                 const float4 x = *reinterpret_cast<const float4*>(p + h * a.logit_stride);
                 const float2 z = s_norm[h];
-                sum.x = fmaf(exp2_of(fmaf(x.x, scale, -z.x)), z.y, sum.x); sum.y = fmaf(exp2_of(fmaf(x.y, scale, -z.x)), z.y, sum.y);
-                sum.z = fmaf(exp2_of(fmaf(x.z, scale, -z.x)), z.y, sum.z); sum.w = fmaf(exp2_of(fmaf(x.w, scale, -z.x)), z.y, sum.w);
+                sum.x = fmaf(exp2_from(x.x, z.x, scale), z.y, sum.x); sum.y = fmaf(exp2_from(x.y, z.x, scale), z.y, sum.y);
+                sum.z = fmaf(exp2_from(x.z, z.x, scale), z.y, sum.z); sum.w = fmaf(exp2_from(x.w, z.x, scale), z.y, sum.w);
             }
         }
         s_sum[threadIdx.x] = sum;

@@ -25,10 +25,10 @@ struct DecodeArgs {
     float* lse;                  // [B, Hq] or NULL
     float* weight;               // [B, weight_stride] or NULL
     int2* pair_workers;          // [pairs]: first and last worker of a (video, kv head, row block)
-    float* part_ml;              // [slots][rows][2]: maximum and sum of a partial result, log2 domain
+    float* part_ml;              // [slots][rows][2]: maximum (before score_scale) and sum of a partial result
     float* part_o;               // [slots][rows][dh]
-    float2* norm;                // [B, Hq]: maximum (log2 domain) and 1 / sum, 0 and 0 without rows, where one worker had all of them
-    float* logits;               // [B, Hq, logit_stride]: without cap before the scale, with cap in the log2 domain
+    float2* norm;                // [B, Hq]: maximum (before score_scale) and 1 / sum, 0 and 0 without rows, where one worker had all of them
+    float* logits;               // [B, Hq, logit_stride], before score_scale
     int64_t weight_stride, logit_stride;
     int B, Hq, Hkv, group, row_blocks, block_rows, rows;
     int S_cap;                   // capacity
@@ -41,6 +41,12 @@ struct DecodeArgs {
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+
+// What takes scores to the log2 domain (capped ones are there), and 2^(score - reference).  The difference is taken before the scale: it is 0 for the
+// reference itself, so that probabilities are relative to the largest one whatever the size of the scores.  (With the scale and the
+// difference in one rounding, to a reference that was rounded at its full size, scores from 2e9 on became 0 or infinite.)
+__device__ __forceinline__ float score_scale(const DecodeArgs& a) { return a.cap > 0.f ? 1.f : a.scale; }
+__device__ __forceinline__ float exp2_from(float score, float reference, float scale) { return exp2_of((score - reference) * scale); }
 
 __device__ __forceinline__ int rows_before(const DecodeArgs& a, int b) {
     const int n = a.len[b];
@@ -362,7 +368,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
 #pragma unroll
                 for (int i = 0; i < NV; ++i) s[nb][i >> 2][i & 3] = a.cap * tanh_of(s[nb][i >> 2][i & 3] * a.scale);
         }
-        const float scale = a.cap > 0.f ? 1.f : a.scale;       // to the log2 domain, rounded once with the difference to the maximum
+        const float scale = score_scale(a);
         if (!f.all) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
@@ -391,9 +397,9 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
             float top = s[nb][0][0];
 #pragma unroll
             for (int i = 1; i < NV; ++i) top = fmaxf(top, s[nb][i >> 2][i & 3]);
-            top = rows_max(top) * scale;
+            top = rows_max(top);
             if (__any(top > m[nb])) {
-                const float to = fmaxf(m[nb], top), g = exp2_of(m[nb] - (to == -INFINITY ? 0.f : to));
+                const float to = fmaxf(m[nb], top), g = exp2_from(m[nb], to == -INFINITY ? 0.f : to, scale);
                 m[nb] = to;
                 l[nb] *= g;
 #pragma unroll
@@ -401,7 +407,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
             }
             const float ref = m[nb] == -INFINITY ? 0.f : m[nb];
 #pragma unroll
-            for (int i = 0; i < NV; ++i) { p[nb][i] = exp2_of(fmaf(s[nb][i >> 2][i & 3], scale, -ref)); l[nb] += p[nb][i]; }
+            for (int i = 0; i < NV; ++i) { p[nb][i] = exp2_from(s[nb][i >> 2][i & 3], ref, scale); l[nb] += p[nb][i]; }
         }
         if constexpr (BF16) {
             // a probability is the sum of two bf16 numbers, 16 of its bits: with one, the result would be as far from the exact one
@@ -460,7 +466,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
             const float sum = swap32_add(swap16_add(l[nb], l[nb]), swap16_add(l[nb], l[nb]));
             const int64_t head = static_cast<int64_t>(x.b) * a.Hq + first_head(x) + 16 * nb + r;
             const int64_t slot = (2 * static_cast<int64_t>(worker) + (begun == 0 ? 1 : 0)) * a.rows + 16 * nb + r;
-            const float lse2 = sum == 0.f ? -INFINITY : m[nb] + log2_of(sum), inv = sum == 0.f ? 0.f : 1.f / sum;
+            const float lse2 = sum == 0.f ? -INFINITY : fmaf(m[nb], score_scale(a), log2_of(sum)), inv = sum == 0.f ? 0.f : 1.f / sum;
             if (whole) {
                 if (r < heads) {
 #pragma unroll
@@ -576,12 +582,12 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
             float top = -INFINITY, total = 0.f;
 #pragma unroll
             for (int w = 0; w < W; ++w) top = fmaxf(top, s_ml[w][row].x);
-            const float ref = top == -INFINITY ? 0.f : top;
+            const float ref = top == -INFINITY ? 0.f : top, scale = score_scale(a);
             float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float2 part = s_ml[w][row];
-                const float f = exp2_of(part.x - ref);
+                const float f = exp2_from(part.x, ref, scale);
                 const float4 v = s_o[((w * kAttendRows + row) * PITCH + 4 * x) / 4];
                 total = fmaf(part.y, f, total);
                 o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
@@ -591,7 +597,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
             char* out = a.out + head * RB + 4 * x * static_cast<int>(sizeof(T));
             if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
             else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-            if (x == 0 && a.lse) a.lse[head] = total == 0.f ? -INFINITY : (ref + log2_of(total)) * 0.693147180559945309f;
+            if (x == 0 && a.lse) a.lse[head] = total == 0.f ? -INFINITY : fmaf(ref, scale, log2_of(total)) * 0.693147180559945309f;
         }
     }
 }

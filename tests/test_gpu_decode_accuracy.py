@@ -54,3 +54,47 @@ def test_the_weights_of_a_step_add_up_to_one(rows, offset, dtype):
     mk().metok_decode_attention(q, k, torch.ones_like(k), lens, weight=w)
     far = (w.double().sum(1) - 1).abs().max().item()
     assert far <= 40 * U, f"{far / U:.1f} u"
+
+
+@pytest.mark.parametrize("rows,weights", FORMS)
+@pytest.mark.parametrize("exponent,cap", [(0, 0.0), (16, 0.0), (32, 0.0), (64, 0.0), (118, 0.0), (0, 2.0 ** 70), (16, 2.0 ** 70), (32, 2.0 ** 70),
+                                          (118, 2.0 ** 70)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_of_any_size(rows, weights, exponent, cap, dtype):
+    """Scores of 2^exponent times 1 to 15, exact in fp32.  From 2^16 on only the largest of a video count, with a probability of 1, and sums of
+    the small whole numbers in V are exact: a quotient's roundings are left.  Scores of 1 to 15 are rounded in the log2 domain, to 21.6 u and,
+    capped, twice, so that probabilities below 1 are off by 30 u at most: those have 0.37 of the sum, the values they draw to are 16
+    apart at most, 0.37 * 30 u * 16 = 178 u, below 8 * 2^-19 = 256 u.  bf16: two parts of a probability are 2^-17 off, and the result is
+    rounded.  A cap of 2^70 leaves scores up to 2^36 as they are and makes those of 2^118 equal: tanh is 1.  The logarithm is a product
+    of three rounded factors, the weights are off as the probabilities are, and by the sum's 7 u."""
+    videos, dh = 3, 64
+    g = torch.Generator().manual_seed(rows + exponent)
+    t = torch.randint(1, 16, (videos, 2, rows), generator=g)
+    v = torch.randint(-8, 9, (videos, 2, rows, dh), generator=g).double()
+    k = torch.zeros((videos, 2, rows, dh), dtype=torch.float64)
+    k[..., 5] = t.double() * 2.0 ** (exponent - exponent // 2)
+    q = torch.zeros((videos, 4, dh), dtype=torch.float64)
+    q[..., 5] = 2.0 ** (exponent // 2)
+    lens = [rows, rows - 1, rows // 2]
+    x = 2.0 ** exponent * t.double()
+    if cap:
+        x = cap * torch.tanh(x / cap)
+    want_w = torch.zeros((videos, rows), dtype=torch.float64)
+    want, lse = torch.zeros((videos, 4, dh), dtype=torch.float64), torch.zeros((videos, 4), dtype=torch.float64)
+    for b, n in enumerate(lens):
+        p = torch.softmax(x[b, :, :n], -1)
+        want_w[b, :n] = p.mean(0)
+        want[b] = torch.matmul(p[:, None], v[b, :, :n])[:, 0].repeat_interleave(2, 0)
+        lse[b] = torch.logsumexp(x[b, :, :n], -1).repeat_interleave(2, 0)
+    to = lambda z: z.to(TORCH[dtype]).cuda()
+    w = torch.zeros((videos, rows), device="cuda")
+    res = mk().metok_decode_attention(to(q), to(k), to(v), torch.tensor(lens, dtype=torch.int32, device="cuda"), scale=1.0, logit_cap=cap,
+                                      weight=w if weights else None)
+    far = (res["out"].double().cpu() - want).abs()
+    if dtype == "bf16":
+        assert (far <= 2.0 ** -8 * want.abs() + 8 * 2.0 ** -15).all(), far.max()
+    else:
+        assert (far <= 8 * 2.0 ** -19).all(), far.max()
+    assert ((res["lse"].double().cpu() - lse).abs() <= 8 * U * (lse.abs() + 1)).all()
+    if weights:
+        assert ((w.double().cpu() - want_w).abs() <= 2.0 ** -18 * want_w + 2.0 ** -126).all()
