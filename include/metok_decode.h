@@ -35,7 +35,7 @@ extern "C" {
  *                cache and attended to.  A video whose cache is full (or whose page for that row is not a page of the pool)
  *                attends to it all the same, but it is not stored.
  *   scale        in [1e-30, 1e30): s_j = scale * (q . k_j); usually 1 / sqrt(dh).  q . k_j and 1.45 s_j have to be finite in fp32.
- *   logit_cap    0: none.  c in [1e-30, 1e30), scale / c < 1e30: s_j becomes c * tanh(s_j / c).
+ *   logit_cap    0: none.  c and scale / c in [1e-30, 1e30): s_j becomes c * tanh(s_j / c).
  *   out          device out, [B, Hq, dh] of `dtype`: sum_j p_j v_j with p = softmax(s) over the video's rows, accumulated in
  *                fp32 and rounded once.  A video without rows gets zeros.
  *   lse          device out, [B, Hq] float, or NULL: log sum_j exp(s_j) (-inf without rows), what two such results are joined by.

@@ -218,7 +218,8 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
     if (!(scale >= 1e-30 && scale < 1e30)) return fail(METOK_ERR_INVALID_ARG, "scale must be positive and finite, in [1e-30, 1e30)");
     if (logit_cap != 0.0 && !(logit_cap >= 1e-30 && logit_cap < 1e30))
         return fail(METOK_ERR_INVALID_ARG, "logit_cap must be 0 (none) or positive and finite, in [1e-30, 1e30)");
-    if (logit_cap != 0.0 && !(scale / logit_cap < 1e30)) return fail(METOK_ERR_INVALID_ARG, "scale / logit_cap must be below 1e30");
+    if (logit_cap != 0.0 && !(scale / logit_cap >= 1e-30 && scale / logit_cap < 1e30))
+        return fail(METOK_ERR_INVALID_ARG, "scale / logit_cap must be in [1e-30, 1e30)");
     if (weight && weight_stride < S_cap) return fail(METOK_ERR_INVALID_ARG, "weight_stride must be at least the capacity");
     const size_t esize = dtype_size(dtype), head = static_cast<size_t>(dh) * esize;
     const AttendPlan plan = plan_attend(B, Hq, Hkv, S_cap, dh, static_cast<int>(esize), weight != nullptr);

@@ -103,6 +103,15 @@ def test_scales_that_fp32_does_not_hold_are_refused(B):
     refused("scale / logit_cap", scale=1e10, cap=1e-25)
 
 
+def test_quotients_of_scale_and_cap_that_fp32_does_not_hold_are_refused(B):
+    """The kernels take tanh of q . k times scale / logit_cap: below fp32's range that factor would lose its bits or be 0, and all scores with it."""
+    for scale, cap in ((1e-25, 1e25), (1e-30, 1.1), (1e-10, 1.1e20), (1e-9, 9e29), (1.01, 1e-30), (1e25, 1e-5)):
+        assert B.lib().metok_decode_attention(*attention_args(scale=scale, cap=cap)) == -1, (scale, cap)
+        assert "scale / logit_cap must" in B.metok_last_error(), B.metok_last_error()
+    for scale, cap in ((1e-30, 1.0), (1e-10, 1e20), (0.125, 9e28), (1e25, 1.1e-5)):         # taken: the workspace is what is missing
+        assert B.lib().metok_decode_attention(*attention_args(scale=scale, cap=cap)) == -3, (scale, cap, B.metok_last_error())
+
+
 def test_refused_paged_attention_calls(B):
     f = B.lib().metok_decode_attention_paged
 
