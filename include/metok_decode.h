@@ -44,7 +44,8 @@ extern "C" {
  *                they were.  weight_stride >= the capacity.
  *   Limits: dh in {32, 64, 128, 256} for bf16, {32, 64, 128} for f32; Hq a multiple of Hkv; 1 <= B <= METOK_MAX_DECODE_BATCH;
  *   Hq <= 1024; capacity below 2^31 - 64; B * Hkv * ceil(Hq / Hkv / 16) * (capacity / 16 + 4) below 2^31.
- *   out, lse and weight must not overlap anything else the call reads or writes.
+ *   out, lse, weight, the workspace and the caches must not overlap each other or anything else the call reads or writes; but K and V may
+ *   be the same cache where no row is appended.
  *   workspace    metok_decode_attention_workspace_bytes(), S_cap being the capacity (pages_per_seq * page_size of a paged cache) and
  *                with_weight whether `weight` is given.  Its contents on entry do not matter.
  * ------------------------------------------------------------------------------------------- */

@@ -112,6 +112,14 @@ def test_quotients_of_scale_and_cap_that_fp32_does_not_hold_are_refused(B):
         assert B.lib().metok_decode_attention(*attention_args(scale=scale, cap=cap)) == -3, (scale, cap, B.metok_last_error())
 
 
+def test_one_cache_for_keys_and_values_is_not_appended_to(B):
+    f = B.lib().metok_decode_attention
+    for v in (FAKE[1], FAKE[1] + 16):
+        assert f(*attention_args(v=v, bytes=1 << 40)) == -1 and "overlaps" in B.metok_last_error()
+    for name in ("out", "lse", "weight", "q", "len", "ws"):                                # and nothing else lies in it when it is only read
+        assert f(*attention_args(v=FAKE[1], k_new=None, v_new=None, bytes=1 << 40, **{name: FAKE[1]})) == -1 and "overlaps" in B.metok_last_error(), name
+
+
 def test_refused_paged_attention_calls(B):
     f = B.lib().metok_decode_attention_paged
 

@@ -140,6 +140,19 @@ def test_a_prefix_of_pages_may_be_shared():
     run(c)
 
 
+@pytest.mark.parametrize("page", [0, 16])
+@pytest.mark.parametrize("capacity", [320, 2048])
+def test_keys_may_be_the_values(page, capacity):
+    """One cache for both, only read: as with a copy of it."""
+    B = mk()
+    c = C.make("bf16", [300, 7], 8, 2, 64, capacity, page, append=False, weights=True, seed=20)
+    for w in (None, c["weight"]):
+        want = C.call(B, c, weight=None if w is None else w.clone()), C.call(B, dict(c, v=c["k"].clone()), weight=None if w is None else w.clone())
+        got = C.call(B, dict(c, v=c["k"]), weight=w)
+        torch.cuda.synchronize()
+        assert C.same(got["out"], want[1]["out"]) and C.same(got["lse"], want[0]["lse"])
+
+
 def test_same_result_every_time_and_on_another_stream():
     B = mk()
     c = C.make("bf16", [3000, 17, 900], 28, 4, 128, 3104, 16, append=True, weights=True, seed=13)
