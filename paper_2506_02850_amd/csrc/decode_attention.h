@@ -1,8 +1,8 @@
 // The kernel that reads the cache for the attention of one new token: for one block of 16 query heads to a kv head at a time (decode.hip),
 // for several (decode_wide.hip), and for short caches in one launch (decode_short.hip).
 //
-// For changes: no instantiation may spill vector registers, and no branch that some lanes take may hold another one.  With both, the compiler
-// has restored a value that all lanes need behind the inner branch, where only some of them are on.
+// For changes: no instantiation may spill vector registers (the build refuses it), and no branch that some lanes take may hold another one.
+// With both, the compiler has restored a value that all lanes need behind the inner branch, where only some of them are on.
 #pragma once
 
 #include "common.h"
