@@ -93,9 +93,12 @@ METOK_API int metok_decode_attention_paged(const void* q, int B, int Hq, int Hkv
  *   reads or writes; of idx, weight, weight_out, len and new_len that is checked.
  * metok_kv_evict and metok_kv_evict_paged select and move the rows of the caches (row i <- row idx[l][b][i]; rows from
  * new_len on are left as they were); metok_kv_evict_select only selects, for callers that relink pages or move the rows themselves.
- *   Paged: rows are moved in place, so pages that videos share may only hold rows that no video moves: among their first n_first ones.
+ *   Paged: one table for all layers (caches relinked by metok_kv_relink_paged, with a table per layer: one call with L = 1 for each, or
+ *   metok_kv_evict_select and metok_kv_relink_paged).  Rows are moved in place, so pages that videos share may only hold rows that no
+ *   video moves: among their first n_first ones.
  *   workspace    metok_kv_evict_workspace_bytes() for the first two, none for the selection; as in metok_kv_compact its first word
- *                is 0 after the call unless a bounded wait expired.
+ *                is 0 after the call unless a bounded wait expired.  Rows were left where they were then, while idx, weight_out and
+ *                new_len are written: the caches are to be given up.
  * ------------------------------------------------------------------------------------------- */
 METOK_API size_t metok_kv_evict_workspace_bytes(int L, int B, int Hkv, int64_t S_cap, int dh, int dtype);
 

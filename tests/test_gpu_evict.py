@@ -360,3 +360,87 @@ def test_pages_shared_among_the_first_rows():
             i, j = np.arange(150), lists[0][b]
             want[table[b, i // page], :, i % page] = old[table[b, j // page], :, j % page]
         np.testing.assert_array_equal(now, want)
+
+
+@pytest.mark.parametrize("page", [0, 8])
+@pytest.mark.parametrize("L", [41, 128])
+def test_more_layers_than_a_launch_of_the_row_mover_takes(L, page):
+    """Budgets and lengths of their own, several tiles a layer, of the 128 every ninth left alone: caches, lists, weights and lengths of all."""
+    B = mk()
+    videos, Hkv, dh, S = 2, 1, 16, 4800
+    rng = np.random.default_rng(L + page)
+    torch.manual_seed(L + page)
+    lens = rng.integers(2000, S + 1, (L, videos)).astype(np.int32)
+    budget = [int(x) for x in rng.integers(200, 4500, L)]
+    alone = set(range(4, L, 9)) if L > 41 else set()
+    w = [weights_of("attention", rng, (videos, S)) for _ in range(L)]
+    lists, new = expected(w, lens, budget, 3, 40, S)
+    for l in alone:
+        new[l] = lens[l]
+    per_seq = S // page if page else 0
+    table = rng.permutation(videos * per_seq).reshape(videos, per_seq).astype(np.int32) if page else None
+    shape = (videos * per_seq, Hkv, page, dh) if page else (videos, Hkv, S, dh)
+    k, v = caches(rng, L, shape, "f32")
+    before = [[bits(t) for t in x] for x in (k, v)]
+    need = B.metok_kv_evict_workspace_bytes(L, videos, Hkv, S, dh, B.F32)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    args = ([None if l in alone else torch.from_numpy(x).cuda() for l, x in enumerate(w)], torch.from_numpy(lens).cuda(), budget, 3, 40)
+    res = B.metok_kv_evict_paged(k, v, torch.from_numpy(table).cuda(), *args, workspace=ws) if page else B.metok_kv_evict(k, v, *args, workspace=ws)
+    torch.cuda.synchronize()
+    assert int(ws[:4].view(torch.int32)[0]) == 0
+    np.testing.assert_array_equal(res["new_len"].cpu().numpy(), new)
+    for l in range(L):
+        if l not in alone:
+            np.testing.assert_array_equal(res["idx"][l].cpu().numpy(), lists[l])
+        for old, now in ((before[0][l], bits(k[l])), (before[1][l], bits(v[l]))):
+            want = old.copy()
+            for b in range(videos):
+                if l in alone:
+                    continue
+                i, j = np.arange(new[l, b]), lists[l][b, :new[l, b]]
+                if page:
+                    want[table[b, i // page], :, i % page] = old[table[b, j // page], :, j % page]
+                else:
+                    want[b][:, i] = old[b][:, j]
+                    got = res["weight"][l].cpu().numpy()
+                    np.testing.assert_array_equal(got[b, i], w[l][b][j])
+            np.testing.assert_array_equal(now, want)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_waits_that_expire_are_reported(page):
+    """Every tile waits for the one before; without polls a wait may be given up: the call ends, says so in the workspace's first word and has replaced
+    lengths and weights.  The next call is whole."""
+    B = mk()
+    Hkv, S, dh, layers = 2, 24000, 128, 2
+    torch.manual_seed(page)
+    weight = torch.rand((1, S), generator=torch.Generator().manual_seed(1)) + 1
+    weight[0, 0] = 0.5                               # the first row leaves, all others move up by one
+    shape = (S // page, Hkv, page, dh) if page else (1, Hkv, S, dh)
+    table = torch.arange(S // page, dtype=torch.int32, device="cuda")[None] if page else None
+    need = B.metok_kv_evict_workspace_bytes(layers, 1, Hkv, S, dh, B.BF16)
+
+    def evict():
+        k, v = caches(None, layers, shape, "bf16")
+        old = [t.clone() for t in k + v]
+        w = [weight.cuda() for _ in range(layers)]
+        lens = torch.full((layers, 1), S, dtype=torch.int32, device="cuda")
+        ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+        args = (w, lens, S - 1)
+        res = (B.metok_kv_evict_paged(k, v, table, *args, new_len=lens, workspace=ws) if page else B.metok_kv_evict(k, v, *args, new_len=lens, workspace=ws))
+        torch.cuda.synchronize()
+        assert lens.tolist() == [[S - 1]] * layers
+        for l in range(layers):
+            assert torch.equal(res["idx"][l][0].cpu(), torch.arange(1, S, dtype=torch.int32)) and torch.equal(w[l][0, :S - 1].cpu(), weight[0, 1:])
+        rows = lambda t: t.transpose(0, 1).reshape(Hkv, S, dh) if page else t[0]
+        moved = all(C.same(rows(t)[:, :S - 1], rows(o)[:, 1:]) and C.same(rows(t)[:, S - 1:], rows(o)[:, S - 1:]) for t, o in zip(k + v, old))
+        return int(ws[:4].view(torch.int32)[0]), moved
+
+    try:
+        B.metok_debug_set_move_spin_limit(0)
+        error, moved = evict()
+        print(f"poll limit 0: error word {error}")
+        assert error == 1 or (error == 0 and moved)
+    finally:
+        B.metok_debug_set_move_spin_limit(1 << 24)
+    assert evict() == (0, True)
