@@ -2,6 +2,9 @@
 import pytest
 import torch
 
+from tests import decode_accuracy as A
+from tests import decode_cases as C
+
 pytestmark = pytest.mark.gpu
 
 U = 2.0 ** -24                                   # half a step of fp32
@@ -98,3 +101,21 @@ def test_scores_of_any_size(rows, weights, exponent, cap, dtype):
     assert ((res["lse"].double().cpu() - lse).abs() <= 8 * U * (lse.abs() + 1)).all()
     if weights:
         assert ((w.double().cpu() - want_w).abs() <= 2.0 ** -18 * want_w + 2.0 ** -126).all()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 32), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("page", [0, 16, 7])
+@pytest.mark.parametrize("rows,weights,Hq,Hkv", [(300, False, 8, 2), (300, True, 8, 2), (4000, False, 8, 2), (4000, True, 14, 2), (700, True, 40, 1), (700, False, 64, 1)])
+def test_errors_are_those_of_fp32(dtype, dh, page, rows, weights, Hq, Hkv):
+    """Ordinary inputs: one launch, split and joined, many query heads; root mean squares as decode_accuracy.py derives them."""
+    capacity = (rows + 10) if page == 0 else page * (-(-(rows + 10) // page))
+    c = C.make(dtype, [rows, rows - 5, rows // 2, 200], Hq, Hkv, dh, capacity, page, append=weights, weights=weights, seed=rows + dh + page)
+    if weights:
+        c["weight"].zero_()
+    res = C.call(mk(), c)
+    keys, values = C.attended(c)
+    got = [res["out"].double().cpu().numpy(), res["lse"].double().cpu().numpy(), None]
+    if weights:
+        w = c["weight"].double().cpu().numpy()
+        got[2] = [w[b, :len(k)] for b, k in enumerate(keys)]
+    assert A.faults(dtype, got, c["q64"], keys, values, dh ** -0.5) == []
