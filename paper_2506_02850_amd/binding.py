@@ -11,6 +11,7 @@ or calling it without a GPU, raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Dict, List, Optional, Sequence
 
@@ -847,7 +848,8 @@ class _Eviction:
         for w in given:
             _shaped(w, "weight[l]", torch.float32, (B, W))
         _shaped(lens, "lens", torch.int32, (L, B))
-        self.budget = [int(budget)] * L if isinstance(budget, int) else [int(x) for x in budget]
+        # a number of any kind (numpy's, too), or one per layer
+        self.budget = [operator.index(budget)] * L if hasattr(budget, "__index__") and not getattr(budget, "ndim", 0) else [operator.index(x) for x in budget]
         if len(self.budget) != L:
             raise ValueError("budget must be one number or one per layer")
         if weight_out is None:

@@ -49,6 +49,20 @@ def test_calls_off_the_gpu_are_declined():
         B.metok_kv_evict_select([w], lens[None], 32, 16)
 
 
+def test_budgets_are_numbers_of_any_kind_or_one_per_layer():
+    import numpy as np
+    w, lens = [torch.zeros(1, 32)] * 2, torch.zeros(2, 1, dtype=torch.int32)
+    for budget in (16, np.int64(16), np.array(16), torch.tensor(16), [16, 8], (np.int32(16), 8), np.array([16, 8]), torch.tensor([16, 8])):
+        with pytest.raises(ValueError, match="GPU"):             # taken: what is wrong is the tensors' place
+            B.metok_kv_evict_select(w, lens, 32, budget)
+    for budget in (16.5, [16, 8.5], "16", None):
+        with pytest.raises(TypeError):
+            B.metok_kv_evict_select(w, lens, 32, budget)
+    for budget in ([16], np.array([16, 8, 4])):
+        with pytest.raises(ValueError, match="budget"):
+            B.metok_kv_evict_select(w, lens, 32, budget)
+
+
 def attention_inputs(paged, dtype=torch.bfloat16):
     g = torch.Generator(device="cuda").manual_seed(3)
     shape = (2, 2, 96, 64) if not paged else (12, 2, 16, 64)
