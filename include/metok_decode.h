@@ -37,15 +37,20 @@ extern "C" {
  *   scale        in [1e-30, 1e30): s_j = scale * (q . k_j); usually 1 / sqrt(dh).  q . k_j and 1.45 s_j have to be finite in fp32.
  *   logit_cap    0: none.  c and scale / c in [1e-30, 1e30): s_j becomes c * tanh(s_j / c).
  *   out          device out, [B, Hq, dh] of `dtype`: sum_j p_j v_j with p = softmax(s) over the video's rows, accumulated in
- *                fp32 and rounded once.  A video without rows gets zeros.
+ *                fp32 and rounded once (with bf16 caches p enters the products as the sum of two bf16 numbers).  A video without rows
+ *                gets zeros.
  *   lse          device out, [B, Hq] float, or NULL: log sum_j exp(s_j) (-inf without rows), what two such results are joined by.
  *   weight       device in/out, [B, weight_stride] float, or NULL: weight[b][j] grows by the mean of p_j over the Hq heads for
- *                every row j that was there before; that of the appended row is set, not added to.  Entries behind the last row are left as
- *                they were.  weight_stride >= the capacity.
+ *                every row j that was there before; that of the new row is set, not added to, where the capacity has a place for it (stored
+ *                or not).  Entries behind the last row are left as they were.  weight_stride >= the capacity.
  *   Limits: dh in {32, 64, 128, 256} for bf16, {32, 64, 128} for f32; Hq a multiple of Hkv; 1 <= B <= METOK_MAX_DECODE_BATCH;
  *   Hq <= 1024; capacity below 2^31 - 64; B * Hkv * ceil(Hq / Hkv / 16) * (capacity / 16 + 4) below 2^31.
  *   out, lse, weight, the workspace and the caches must not overlap each other or anything else the call reads or writes; but K and V may
  *   be the same cache where no row is appended.
+ *   The work is split by the capacity, not by the lengths, which are on the device: with short requests in paged caches a page_table no wider
+ *   than they need is faster (capacities up to 1023 rows in bf16, 511 for heads of 256 and in fp32, take one launch without weights
+ *   and with at most 16 query heads to a kv head).
+ *   A video that is not there (padding of a batch) has a length of 0 and, where a row is appended, no pages in its table.
  *   workspace    metok_decode_attention_workspace_bytes(), S_cap being the capacity (pages_per_seq * page_size of a paged cache) and
  *                with_weight whether `weight` is given.  Its contents on entry do not matter.
  * ------------------------------------------------------------------------------------------- */

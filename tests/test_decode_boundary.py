@@ -152,6 +152,22 @@ def test_workspace_sizes(B):
         assert f(*bad) == 0
 
 
+def test_the_workspace_of_partial_results(B):
+    """Two of a maximum, a sum and an output in fp32 for each of 1024 waves (2048 where a tile of K and V is 4 KB) and each query head that it takes at a
+    time, whatever the batch and the capacity: 67.6 MB at most; and 8 bytes per (video, kv head, turn of its query heads)."""
+    f, most = B.metok_decode_attention_workspace_bytes, 0
+    for dtype, dh in ((B.BF16, 32), (B.BF16, 64), (B.BF16, 128), (B.BF16, 256), (B.F32, 32), (B.F32, 64), (B.F32, 128)):
+        waves = 2048 if dh == 32 else 1024
+        for group in (1, 7, 16, 17, 31, 32, 33, 40, 64, 65, 128, 1000, 1024):
+            turn = 16 if group <= 16 else 64 if dh <= 64 and group > 32 else 32
+            parts = 2 * waves * min(group, turn) * (dh + 2) * 4
+            most = max(most, parts)
+            for videos, capacity in ((1, 5000), (8, 100000), (64, 5000)):
+                pairs = videos * -(-group // turn)
+                assert f(videos, group, 1, capacity, dh, dtype) == parts + -(-8 * pairs // 256) * 256, (dtype, dh, group)
+    assert most == 2 * 1024 * 32 * 258 * 4 == 67633152
+
+
 PLAN = r"""
 #include <initializer_list>
 #include "decode_plan.h"
