@@ -9,7 +9,7 @@
 // What bounds it is the stream of K and V: 4 Hq dh operations a row on 2 Hkv dh elements, 7 operations a byte with seven query
 // heads to a kv head in bf16.  The query heads of a kv head are the columns of one MFMA, so a row is read once for all of them.
 // 8 videos of 36992 rows, 28 heads on 4 of 128 in bf16, 606 MB: 95.5 us a call, 6.35 TB/s (the join 4.5 us of it; a copy of 1 GiB moves
-// 6.65 TB/s).  One of 2306 rows 8.6 us: two launches and their latency.
+// 6.65 TB/s).  One of 2306 rows 8.8 us: two launches and their latency.
 #include "decode_attention.h"
 
 namespace metok {

@@ -9,7 +9,8 @@ namespace metok {
 constexpr int kAttendWaves = 4, kAttendThreads = 64 * kAttendWaves;
 constexpr int kAttendRows = 16;                // query rows of a block: one MFMA's columns
 // Blocks of a wave where a kv head has more than one: four where they fit the registers beside K, V and the sums and more than two are there
-// (8 x 149990 rows of 64 elements, 24 query heads on one kv head: 82 us with four, 62 with two; 48 of them 81 and 93; 71 of them 141 and 159).
+// (8 x 149990 rows of 64 elements, 24 query heads on one kv head: 85 us with four, 62 with two; 48 of them 84 and 97; 71 of them 147 and 159, but 48
+// and 44 with 36990 rows, which stay in the caches between the turns).
 constexpr int attend_blocks(int dh, int group) { return dh <= 64 && group > 2 * kAttendRows ? 4 : 2; }
 // Cache rows of a tile: K and V of the next one are on their way in registers, 64 of them at most.
 constexpr int attend_tile(int esize, int dh) { return esize * dh <= 256 && esize == 2 ? 32 : 16; }
