@@ -26,6 +26,7 @@ SIM_FLAT, SIM_TOKEN_MEAN, SIM_POOLED = 0, 1, 2
 SCORE_CAUSAL_ALL, SCORE_VISUAL_ONLY = 0, 1
 EVENT_MEAN, EVENT_MAX = 0, 1
 POOL_FLOOR, POOL_CEIL = 0, 1
+PAIRS_HALVES, PAIRS_ADJACENT = 0, 1
 
 EXPORTS = [
     "metok_last_error", "metok_version",
@@ -46,6 +47,11 @@ EXPORTS = [
 DECODE_EXPORTS = [
     "metok_decode_attention_workspace_bytes", "metok_decode_attention", "metok_decode_attention_paged",
     "metok_kv_evict_workspace_bytes", "metok_kv_evict", "metok_kv_evict_paged", "metok_kv_evict_select",
+]
+# those of metok_qkv.h
+QKV_EXPORTS = [
+    "metok_rotate_qk", "metok_rotate_qk_paged", "metok_kv4_cache_bytes", "metok_kv4_pack", "metok_kv4_pack_paged", "metok_kv4_unpack", "metok_kv4_unpack_paged",
+    "metok_kv4_attention_workspace_bytes", "metok_kv4_attention", "metok_kv4_attention_paged",
 ]
 
 
@@ -159,6 +165,23 @@ def _load() -> ctypes.CDLL:
     lib.metok_kv_evict_paged.argtypes = [vpp, vpp, i32, i32, i32, i64, i32, i32, i32, vp, i32, vpp, vpp, i64] + select_tail + [vp, sz, vp]
     lib.metok_kv_evict_select.restype = i32
     lib.metok_kv_evict_select.argtypes = [vpp, vpp, i64, i32, i32, i64] + select_tail + [vp]
+    rotate_head = [vp, vp, vp, i64, i64, i64, i32, i64, i32, i32, i32, i32, vp, vp, vp, dbl, vp, i32, vp, c.c_char_p, i32, i32, vp, vp, vp]
+    lib.metok_rotate_qk.argtypes = rotate_head + [i64, vp, vp]
+    lib.metok_rotate_qk_paged.argtypes = rotate_head + [i64, i32, vp, i32, vp, vp]
+    lib.metok_kv4_cache_bytes.restype = sz
+    lib.metok_kv4_cache_bytes.argtypes = [i64, i32, i64, i32]
+    pack_head = [vp, vp, i32, i32, i64, i32, i32, vp, i64, vp, vp, vp]
+    lib.metok_kv4_pack.argtypes = pack_head + [i64, vp, vp]
+    lib.metok_kv4_pack_paged.argtypes = pack_head + [i64, i32, vp, i32, vp, vp]
+    unpack_tail = [vp, vp, vp, i64, vp, vp, i64, i32, vp]
+    lib.metok_kv4_unpack.argtypes = [vp, vp, i32, i32, i64, i32] + unpack_tail
+    lib.metok_kv4_unpack_paged.argtypes = [vp, vp, i32, i32, i64, i32, i32, vp, i32] + unpack_tail
+    lib.metok_kv4_attention_workspace_bytes.restype = sz
+    lib.metok_kv4_attention_workspace_bytes.argtypes = lib.metok_decode_attention_workspace_bytes.argtypes
+    lib.metok_kv4_attention.argtypes = lib.metok_decode_attention.argtypes
+    lib.metok_kv4_attention_paged.argtypes = lib.metok_decode_attention_paged.argtypes
+    for name in ("rotate_qk", "rotate_qk_paged", "kv4_pack", "kv4_pack_paged", "kv4_unpack", "kv4_unpack_paged", "kv4_attention", "kv4_attention_paged"):
+        getattr(lib, "metok_" + name).restype = i32
     return lib
 
 
@@ -760,24 +783,32 @@ def metok_decode_attention_workspace_bytes(B: int, Hq: int, Hkv: int, S_cap: int
     return int(_lib.metok_decode_attention_workspace_bytes(int(B), int(Hq), int(Hkv), int(S_cap), int(dh), int(dtype_code), int(bool(with_weight))))
 
 
-def _decode_attention(q, k, v, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out) -> Dict[str, torch.Tensor]:
+def _cache_shape(four: bool, rows: int, dh: int):
+    """What follows the heads in the shape of a cache of so many rows."""
+    return (rows // 16, 17 * dh // 2) if four else (rows, dh)
+
+
+def _decode_attention(q, k, v, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, four=False) -> Dict[str, torch.Tensor]:
+    """four: over a cache in 4 bits."""
     _dev(q, "q")
     if q.dim() != 3 or k.dim() != 4 or k.shape != v.shape:
         raise ValueError("q must be [B, Hq, dh], K and V of one 4-dimensional shape")
     B, Hq, dh = q.shape
-    dt, dev = _dtype_code(q), q.device
+    dt, dev, held, block = _dtype_code(q), q.device, torch.uint8 if four else q.dtype, 16 if four else 1
+    call, call_paged, workspace_bytes = ((_lib.metok_kv4_attention, _lib.metok_kv4_attention_paged, _lib.metok_kv4_attention_workspace_bytes) if four else
+                                         (_lib.metok_decode_attention, _lib.metok_decode_attention_paged, _lib.metok_decode_attention_workspace_bytes))
     if page_table is None:
-        Hkv, S_cap = int(k.shape[1]), int(k.shape[2])
-        _shaped(k, "k_cache", q.dtype, (B, Hkv, S_cap, dh))
+        Hkv, S_cap = int(k.shape[1]), int(k.shape[2]) * block
+        _shaped(k, "k_cache", held, (B, Hkv, *_cache_shape(four, S_cap, dh)))
     else:
-        n_pages, Hkv, page_size = (int(x) for x in k.shape[:3])
-        _shaped(k, "k_pool", q.dtype, (n_pages, Hkv, page_size, dh))
+        n_pages, Hkv, page_size = int(k.shape[0]), int(k.shape[1]), int(k.shape[2]) * block
+        _shaped(k, "k_pool", held, (n_pages, Hkv, *_cache_shape(four, page_size, dh)))
         if page_table.dim() != 2:
             raise ValueError("page_table must be int32 [B, pages_per_seq]")
         pages_per_seq = int(page_table.shape[1])
         _shaped(page_table, "page_table", torch.int32, (B, pages_per_seq))
         S_cap = pages_per_seq * page_size
-    _shaped(v, "V", q.dtype, k.shape)
+    _shaped(v, "V", held, k.shape)
     _shaped(lens, "lens", torch.int32, (B,))
     if (k_new is None) != (v_new is None):
         raise ValueError("k_new and v_new go together")
@@ -790,15 +821,15 @@ def _decode_attention(q, k, v, page_table, lens, k_new, v_new, scale, logit_cap,
                        **{f"out[{n!r}]": t for n, t in (out or {}).items()})
     result = dict(out=_out(out, "out", (B, Hq, dh), q.dtype, dev), lse=_out(out, "lse", (B, Hq), torch.float32, dev))
     ws = workspace if workspace is not None else _workspace(
-        _lib.metok_decode_attention_workspace_bytes(B, Hq, Hkv, S_cap, dh, dt, int(weight is not None)), dev)
+        workspace_bytes(B, Hq, Hkv, S_cap, dh, dt, int(weight is not None)), dev)
     scale = dh ** -0.5 if scale is None else float(scale)
     tail = (_dev(lens, "lens"), _dev(k_new, "k_new"), _dev(v_new, "v_new"), scale, float(logit_cap), _dev(result["out"], "out"), _dev(result["lse"], "lse"),
             _dev(weight, "weight"), weight.shape[1] if weight is not None else 0, _dev(ws, "workspace"), ws.numel() * ws.element_size(), _stream())
     if page_table is None:
-        _check(_lib.metok_decode_attention(_dev(q, "q"), B, Hq, Hkv, dh, dt, _dev(k, "k_cache"), _dev(v, "v_cache"), S_cap, *tail))
+        _check(call(_dev(q, "q"), B, Hq, Hkv, dh, dt, _dev(k, "k_cache"), _dev(v, "v_cache"), S_cap, *tail))
     else:
-        _check(_lib.metok_decode_attention_paged(_dev(q, "q"), B, Hq, Hkv, dh, dt, _dev(k, "k_pool"), _dev(v, "v_pool"), n_pages, page_size,
-                                                 _dev(page_table, "page_table"), pages_per_seq, *tail))
+        _check(call_paged(_dev(q, "q"), B, Hq, Hkv, dh, dt, _dev(k, "k_pool"), _dev(v, "v_pool"), n_pages, page_size,
+                          _dev(page_table, "page_table"), pages_per_seq, *tail))
     return result
 
 
@@ -957,6 +988,214 @@ def metok_kv_evict_select(weight: Sequence[Optional[torch.Tensor]], lens: torch.
     e = _Eviction(weight, lens, budget, weight_out, idx, new_len)
     _check(_lib.metok_kv_evict_select(*e.weights, e.L, e.B, int(S_cap), *e.lengths, int(n_first), int(n_last), *e.outputs, _stream()))
     return e.result()
+
+
+# ---- queries, keys and values of new tokens; caches in 4 bits (metok_qkv.h) ----
+def _pages(page_table: Optional[torch.Tensor], B: int):
+    """B, as the page table of a paged call has it."""
+    if page_table is None or page_table.dim() != 2:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    _shaped(page_table, "page_table", torch.int32, (B, int(page_table.shape[1])))
+    return _dev(page_table, "page_table"), int(page_table.shape[1])
+
+
+def _per_video(t: Optional[torch.Tensor], name: str, B: int) -> Optional[int]:
+    return None if t is None else _dev(_shaped(t, name, torch.int32, (B,)), name)
+
+
+def _token_rows(t: torch.Tensor, name: str, dtype: torch.dtype, B: int, n: int, dh: int):
+    """Address, heads and elements between tokens of q, k or v [B, n, heads, dh], which may be a part of a wider buffer."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU (there is no CPU path)")
+    if t.dim() != 4 or t.dtype != dtype or t.shape[0] != B or t.shape[1] != n or t.shape[3] != dh:
+        raise ValueError(f"{name} must be {dtype} of shape [{B}, {n}, heads, {dh}], got {t.dtype} {tuple(t.shape)}")
+    heads = int(t.shape[2])
+    stride = t.stride(1) if n > 1 else t.stride(0) if B > 1 else heads * dh
+    if t.stride(3) != 1 or (heads > 1 and t.stride(2) != dh) or (B > 1 and t.stride(0) != n * stride):
+        raise ValueError(f"{name}: a token's heads must lie beside each other, and its tokens at one distance")
+    return t.data_ptr(), heads, stride
+
+
+def _rotate_qk(q, k, v, pos, inv_freq, k_cache, v_cache, page_table, start, count, pair_axis, q_weight, k_weight, eps, pairs, out) -> Dict[str, torch.Tensor]:
+    if q.dim() != 4 or k_cache.dim() != 4:
+        raise ValueError("q must be [B, n, Hq, dh] and the caches 4-dimensional")
+    B, n, _, dh = (int(x) for x in q.shape)
+    dt = _dtype_code(q)
+    (qp, Hq, qs), (kp, Hkv, ks), (vp, Hv, vs) = (_token_rows(t, name, q.dtype, B, n, dh) for t, name in ((q, "q"), (k, "k"), (v, "v")))
+    if Hv != Hkv:
+        raise ValueError("k and v must have as many heads")
+    if page_table is None:
+        _shaped(k_cache, "k_cache", q.dtype, (B, Hkv, int(k_cache.shape[2]), dh))
+    else:
+        _shaped(k_cache, "k_pool", q.dtype, (int(k_cache.shape[0]), Hkv, int(k_cache.shape[2]), dh))
+    _shaped(v_cache, "V", q.dtype, k_cache.shape)
+    if pos.dim() == 2:
+        pos = pos[None]
+    n_axes = int(pos.shape[0])
+    _shaped(pos, "pos", torch.int32, (n_axes, B, n))
+    if inv_freq.dim() != 1:
+        raise ValueError("inv_freq must be float32 [rot / 2]")
+    half = int(inv_freq.shape[0])
+    _shaped(inv_freq, "inv_freq", torch.float32, (half,))
+    if pair_axis is not None:
+        pair_axis = bytes(pair_axis)
+        if len(pair_axis) != half:
+            raise ValueError("pair_axis must have an axis for each entry of inv_freq")
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _shaped(t, name, q.dtype, (dh,))
+    _on_current_device(q=q, k=k, v=v, pos=pos, inv_freq=inv_freq, k_cache=k_cache, v_cache=v_cache, page_table=page_table, start=start, count=count,
+                       q_weight=q_weight, k_weight=k_weight, **{f"out[{x!r}]": t for x, t in (out or {}).items()})
+    q_out = _out(out, "q", (B, Hq, n, dh), q.dtype, q.device)
+    head = (qp, kp, vp, qs, ks, vs, B, n, Hq, Hkv, dh, dt, _per_video(count, "count", B), _dev(q_weight, "q_weight"), _dev(k_weight, "k_weight"), float(eps),
+            _dev(pos, "pos"), n_axes, _dev(inv_freq, "inv_freq"), pair_axis, 2 * half, int(pairs), _dev(q_out, "out['q']"), _dev(k_cache, "k_cache"), _dev(v_cache, "v_cache"))
+    rows, start = int(k_cache.shape[2]), _per_video(start, "start", B)
+    if page_table is None:
+        _check(_lib.metok_rotate_qk(*head, rows, start, _stream()))
+    else:
+        _check(_lib.metok_rotate_qk_paged(*head, int(k_cache.shape[0]), rows, *_pages(page_table, B), start, _stream()))
+    return dict(q=q_out)
+
+
+def metok_rotate_qk(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                    start: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, pair_axis: Optional[bytes] = None,
+                    q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, pairs: int = PAIRS_HALVES,
+                    out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """New tokens' q [B, n, Hq, dh], k and v [B, n, Hkv, dh] (parts of one buffer are fine): q and k are normed for each head where the weights [dh] are
+    given and rotated by the positions pos [axes, B, n] int32 (or [B, n]), pair p of a head's first 2 * len(inv_freq) elements by pos[pair_axis[p]] *
+    inv_freq[p]; k and v become rows start[b] + i of the cache [B, Hkv, S_cap, dh].  count [B]: tokens that video b has.  Returns q [B, Hq, n, dh]
+    (of tokens that are not there: whatever the tensor held); `out` may carry it."""
+    return _rotate_qk(q, k, v, pos, inv_freq, k_cache, v_cache, None, start, count, pair_axis, q_weight, k_weight, eps, pairs, out)
+
+
+def metok_rotate_qk_paged(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor,
+                          page_table: torch.Tensor, start: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, pair_axis: Optional[bytes] = None,
+                          q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, pairs: int = PAIRS_HALVES,
+                          out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """metok_rotate_qk into one layer's pools [n_pages, Hkv, page_size, dh] through page_table [B, pages_per_seq]."""
+    if page_table is None:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    return _rotate_qk(q, k, v, pos, inv_freq, k_pool, v_pool, page_table, start, count, pair_axis, q_weight, k_weight, eps, pairs, out)
+
+
+def metok_kv4_cache_bytes(B: int, Hkv: int, S_cap: int, dh: int) -> int:
+    return int(_lib.metok_kv4_cache_bytes(int(B), int(Hkv), int(S_cap), int(dh)))
+
+
+def metok_kv4_cache(B: int, Hkv: int, S_cap: int, dh: int, device) -> List[torch.Tensor]:
+    """K and V of an empty 4-bit cache of S_cap rows (a multiple of 16) for each of B videos; n_pages, Hkv, page_size for pools."""
+    if metok_kv4_cache_bytes(B, Hkv, S_cap, dh) == 0:
+        raise ValueError("metok_kv4_cache: arguments out of range")
+    return [torch.empty((B, Hkv, *_cache_shape(True, S_cap, dh)), dtype=torch.uint8, device=device) for _ in range(2)]
+
+
+def _cache4(k: torch.Tensor, v: torch.Tensor, slabs: Optional[int], Hkv: Optional[int], dh: Optional[int]):
+    """Addresses, slabs, kv heads, rows and elements of a 4-bit cache or pool."""
+    if k.dim() != 4:
+        raise ValueError("a 4-bit cache must be 4-dimensional")
+    dh = int(k.shape[3]) * 2 // 17 if dh is None else dh
+    slabs = int(k.shape[0]) if slabs is None else slabs
+    Hkv = int(k.shape[1]) if Hkv is None else Hkv
+    _shaped(k, "the 4-bit K", torch.uint8, (slabs, Hkv, *_cache_shape(True, 16 * int(k.shape[2]), dh)))
+    _shaped(v, "the 4-bit V", torch.uint8, k.shape)
+    return _dev(k, "the 4-bit K"), _dev(v, "the 4-bit V"), slabs, Hkv, 16 * int(k.shape[2]), dh
+
+
+def _kv4_pack(k, v, k4, v4, page_table, start, count, idx) -> None:
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+        raise ValueError("k and v must be of one 4-dimensional shape and type")
+    B, Hkv, S_src, dh = (int(x) for x in k.shape)
+    dt = _dtype_code(k)
+    kp, vp, slabs, _, rows, _ = _cache4(k4, v4, B if page_table is None else None, Hkv, dh)
+    n = S_src
+    if idx is not None:
+        if idx.dim() != 2:
+            raise ValueError("idx must be int32 [B, n]")
+        n = int(idx.shape[1])
+        _shaped(idx, "idx", torch.int32, (B, n))
+    _on_current_device(k=k, v=v, k_cache=k4, v_cache=v4, page_table=page_table, start=start, count=count, idx=idx)
+    head = (_dev(k, "k"), _dev(v, "v"), B, Hkv, S_src, dh, dt, _dev(idx, "idx"), n, _per_video(count, "count", B), kp, vp)
+    start = _per_video(start, "start", B)
+    if page_table is None:
+        _check(_lib.metok_kv4_pack(*head, rows, start, _stream()))
+    else:
+        _check(_lib.metok_kv4_pack_paged(*head, slabs, rows, *_pages(page_table, B), start, _stream()))
+
+
+def metok_kv4_pack(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, start: Optional[torch.Tensor] = None,
+                   count: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None) -> None:
+    """Rows of k, v [B, Hkv, S_src, dh] into a 4-bit cache (metok_kv4_cache): row start[b] + i receives source row i, or idx[b][i] of idx [B, n], for
+    i < count[b]; the cache's other rows stay as they were."""
+    _kv4_pack(k, v, k_cache, v_cache, None, start, count, idx)
+
+
+def metok_kv4_pack_paged(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor,
+                         start: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, idx: Optional[torch.Tensor] = None) -> None:
+    """metok_kv4_pack into 4-bit pools (metok_kv4_cache of n_pages, Hkv, page_size, dh) through page_table [B, pages_per_seq]."""
+    if page_table is None:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    _kv4_pack(k, v, k_pool, v_pool, page_table, start, count, idx)
+
+
+def _kv4_unpack(k4, v4, page_table, lens, n, first, idx, dtype, out) -> Dict[str, torch.Tensor]:
+    B = int(lens.shape[0]) if lens.dim() == 1 else -1
+    kp, vp, slabs, Hkv, rows, dh = _cache4(k4, v4, B if page_table is None else None, None, None)
+    if idx is not None:
+        _shaped(idx, "idx", torch.int32, (B, int(n)))
+    _on_current_device(k_cache=k4, v_cache=v4, page_table=page_table, lens=lens, first=first, idx=idx, **{f"out[{x!r}]": t for x, t in (out or {}).items()})
+    given = [out[x] for x in ("k", "v") if out is not None and out.get(x) is not None]
+    S_out = int(n)
+    if given:
+        if given[0].dim() != 4:
+            raise ValueError("out['k'] and out['v'] must be [B, Hkv, S_out, dh]")
+        dtype, S_out = given[0].dtype, int(given[0].shape[2])
+    result = {x: _out(out, x, (B, Hkv, S_out, dh), dtype, k4.device) for x in ("k", "v")}
+    tail = (_per_video(lens, "lens", B), _per_video(first, "first", B), _dev(idx, "idx"), int(n), _dev(result["k"], "out['k']"), _dev(result["v"], "out['v']"), S_out,
+            _dtype_code(result["k"]), _stream())
+    if page_table is None:
+        _check(_lib.metok_kv4_unpack(kp, vp, B, Hkv, rows, dh, *tail))
+    else:
+        _check(_lib.metok_kv4_unpack_paged(kp, vp, B, Hkv, slabs, rows, dh, *_pages(page_table, B), *tail))
+    return result
+
+
+def metok_kv4_unpack(k_cache: torch.Tensor, v_cache: torch.Tensor, lens: torch.Tensor, n: int, first: Optional[torch.Tensor] = None,
+                     idx: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """n rows of every video of a 4-bit cache as the values they stand for: row i is row first[b] + i, or idx[b][i] of idx [B, n], where that is below lens[b];
+    other rows of the outputs are not written.  Returns k and v [B, Hkv, n, dh] of dtype; `out` may carry them, with more rows, too."""
+    return _kv4_unpack(k_cache, v_cache, None, lens, n, first, idx, dtype, out)
+
+
+def metok_kv4_unpack_paged(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, n: int, first: Optional[torch.Tensor] = None,
+                           idx: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                           out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """metok_kv4_unpack of 4-bit pools through page_table [B, pages_per_seq]."""
+    if page_table is None:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    return _kv4_unpack(k_pool, v_pool, page_table, lens, n, first, idx, dtype, out)
+
+
+def metok_kv4_attention_workspace_bytes(B: int, Hq: int, Hkv: int, S_cap: int, dh: int, dtype_code: int, with_weight: bool = False) -> int:
+    return int(_lib.metok_kv4_attention_workspace_bytes(int(B), int(Hq), int(Hkv), int(S_cap), int(dh), int(dtype_code), int(bool(with_weight))))
+
+
+def metok_kv4_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, lens: torch.Tensor,
+                        k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                        scale: Optional[float] = None, logit_cap: float = 0.0, weight: Optional[torch.Tensor] = None,
+                        workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """metok_decode_attention over a 4-bit cache (metok_kv4_cache).  k_new / v_new [B, Hkv, dh], of q's type, are put into 4 bits, stored at row lens[b]
+    and attended to as what is stored."""
+    return _decode_attention(q, k_cache, v_cache, None, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, four=True)
+
+
+def metok_kv4_attention_paged(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor,
+                              k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                              scale: Optional[float] = None, logit_cap: float = 0.0, weight: Optional[torch.Tensor] = None,
+                              workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """metok_kv4_attention over 4-bit pools through page_table [B, pages_per_seq]."""
+    if page_table is None:
+        raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    return _decode_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, four=True)
 
 
 def metok_debug_set_move_spin_limit(polls: int) -> None:

@@ -37,6 +37,20 @@ struct TraceScope {
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 inline size_t dtype_size(int dtype) { return dtype == METOK_BF16 ? 2 : 4; }
+// A buffer of a call, for the checks of what must not overlap.
+struct Span { const char* name; const void* p; size_t bytes; };
+inline bool overlap(const Span& x, const Span& y) {
+    if (!x.p || !y.p || !x.bytes || !y.bytes) return false;
+    const char *a = static_cast<const char*>(x.p), *b = static_cast<const char*>(y.p);
+    return a < b + y.bytes && b < a + x.bytes;
+}
+// None of the first `written` overlaps any other: METOK_OK, or the refusal.
+inline int check_spans(const Span* spans, int written, int n) {
+    for (int i = 0; i < written; ++i)
+        for (int j = i + 1; j < n; ++j)
+            if (overlap(spans[i], spans[j])) return fail(METOK_ERR_INVALID_ARG, "%s overlaps %s", spans[i].name, spans[j].name);
+    return METOK_OK;
+}
 int ceil_ratio(double x);                   // ceil(x - 1e-9)
 
 // Lets a kernel have `bytes` of dynamic LDS (the same for each of its launches): beyond 64 KB by an attribute of the current device's copy of it.

@@ -159,7 +159,7 @@ __global__ __launch_bounds__(kJoinThreads) void decode_join_kernel(const DecodeA
 constexpr int64_t kStreamBytes = 128 << 20;
 
 template <typename T, int DH>
-static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) {
+static int launch_attend(const DecodeArgs& a, const AttendPlan& plan, hipStream_t st) {
     const int64_t bytes = static_cast<int64_t>(a.B) * a.Hkv * a.S_cap * DH * static_cast<int64_t>(sizeof(T)) * 2;
     const unsigned groups = static_cast<unsigned>(plan.grid);
     const bool stream = bytes > kStreamBytes;
@@ -171,8 +171,22 @@ static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) 
     else if (!a.table) stream ? launch_attention<T, DH, kDense, true, 1>(a, groups, st) : launch_attention<T, DH, kDense, false, 1>(a, groups, st);
     else if (a.page_size % 16 != 0) stream ? launch_attention<T, DH, kRows, true, 1>(a, groups, st) : launch_attention<T, DH, kRows, false, 1>(a, groups, st);
     else stream ? launch_attention<T, DH, kBlocks, true, 1>(a, groups, st) : launch_attention<T, DH, kBlocks, false, 1>(a, groups, st);
-    int rc = check_launch("decode attention");
-    if (rc) return rc;
+    return check_launch("decode attention");
+}
+static int launch_decode(const DecodeArgs& a, const AttendPlan& plan, int dtype, int dh, hipStream_t st) {
+    if (dtype == METOK_BF16) {
+        if (dh == 32) return launch_attend<bf16_t, 32>(a, plan, st);
+        if (dh == 64) return launch_attend<bf16_t, 64>(a, plan, st);
+        if (dh == 128) return launch_attend<bf16_t, 128>(a, plan, st);
+        return launch_attend<bf16_t, 256>(a, plan, st);
+    }
+    if (dh == 32) return launch_attend<float, 32>(a, plan, st);
+    if (dh == 64) return launch_attend<float, 64>(a, plan, st);
+    return launch_attend<float, 128>(a, plan, st);
+}
+
+template <typename T, int DH>
+static int launch_join(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) {
     const int64_t units = plan.joined ? static_cast<int64_t>(a.B) * a.Hq : 0;
     // few heads have many parts each: their elements over several workgroups
     a.join_lanes = units * (DH / 4 / 8) <= kJoinSpread ? 8 : DH / 4;
@@ -185,29 +199,25 @@ static int launch_attend(DecodeArgs& a, const AttendPlan& plan, hipStream_t st) 
     return check_launch("decode join");
 }
 
-// The shapes that the calls and the workspace query take, NULL or the reason why not.
-static const char* bad_shape(int B, int Hq, int Hkv, int64_t S_cap, int dh, int dtype) {
+const char* bad_attend_heads(int B, int Hq, int Hkv, int dh, int dtype) {
     if (dtype != METOK_F32 && dtype != METOK_BF16) return "unknown dtype";
     if (B < 1 || B > METOK_MAX_DECODE_BATCH) return "B must be in [1, METOK_MAX_DECODE_BATCH]";
     if (Hkv < 1 || Hq < 1 || Hq > 1024 || Hq % Hkv != 0) return "Hq must be a multiple of Hkv and at most 1024";
     if (dh != 32 && dh != 64 && dh != 128 && !(dh == 256 && dtype == METOK_BF16)) return "dh must be 32, 64, 128 or (bf16) 256";
+    return nullptr;
+}
+// The shapes that the calls and the workspace query take, NULL or the reason why not.
+static const char* bad_shape(int B, int Hq, int Hkv, int64_t S_cap, int dh, int dtype) {
+    if (const char* why = bad_attend_heads(B, Hq, Hkv, dh, dtype)) return why;
     if (S_cap < 1 || S_cap >= INT32_MAX - 64) return "the capacity must be in [1, 2^31 - 64)";
     const int64_t pairs = static_cast<int64_t>(B) * Hkv * ((Hq / Hkv + kAttendRows - 1) / kAttendRows);      // at most
     if (pairs * (S_cap / 16 + 4) > INT32_MAX) return "too many rows";
     return nullptr;
 }
 
-struct Span { const char* name; const void* p; size_t bytes; };
-static bool overlap(const Span& x, const Span& y) {
-    if (!x.p || !y.p || !x.bytes || !y.bytes) return false;
-    const char *a = static_cast<const char*>(x.p), *b = static_cast<const char*>(y.p);
-    return a < b + y.bytes && b < a + x.bytes;
-}
-
-static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype, void* k, void* v, int64_t S_cap, size_t cache_bytes,
-                       const int32_t* table, int64_t n_pages, int page_size, int pages_per_seq, const int32_t* len,
-                       const void* k_new, const void* v_new, double scale, double logit_cap,
-                       void* out, float* lse, float* weight, int64_t weight_stride, void* workspace, size_t workspace_bytes, void* stream) {
+int attend_call(const AttendCall& c, const AttendPlan& plan, int (*launch)(const DecodeArgs& a, const AttendPlan& plan, int dtype, int dh, hipStream_t st)) {
+    const auto& [q, B, Hq, Hkv, dh, dtype, k, v, S_cap, cache_bytes, table, n_pages, page_size, pages_per_seq, len, k_new, v_new, scale, logit_cap,
+                 out, lse, weight, weight_stride, workspace, workspace_bytes, stream] = c;
     if (!q || !k || !v || !len || !out) return fail(METOK_ERR_INVALID_ARG, "q, the caches, len and out must not be NULL");
     if ((k_new == nullptr) != (v_new == nullptr)) return fail(METOK_ERR_INVALID_ARG, "k_new and v_new go together");
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out))
@@ -222,7 +232,6 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
         return fail(METOK_ERR_INVALID_ARG, "scale / logit_cap must be in [1e-30, 1e30)");
     if (weight && weight_stride < S_cap) return fail(METOK_ERR_INVALID_ARG, "weight_stride must be at least the capacity");
     const size_t esize = dtype_size(dtype), head = static_cast<size_t>(dh) * esize;
-    const AttendPlan plan = plan_attend(B, Hq, Hkv, S_cap, dh, static_cast<int>(esize), weight != nullptr);
     if (plan.bytes && (!workspace || workspace_bytes < plan.bytes || !aligned16(workspace)))
         return fail(METOK_ERR_WORKSPACE, "workspace of %zu bytes needed (16-byte aligned), %zu given", plan.bytes, workspace_bytes);
     const Span spans[] = {
@@ -258,15 +267,16 @@ static int attend_impl(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
     const int64_t most = (S_cap + kWeightRows - 1) / kWeightRows, enough = (1024 + B - 1) / B;
     a.weight_blocks = static_cast<int>(most < enough ? most : enough);
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (int rc = launch(a, plan, dtype, dh, st)) return rc;
     if (dtype == METOK_BF16) {
-        if (dh == 32) return launch_attend<bf16_t, 32>(a, plan, st);
-        if (dh == 64) return launch_attend<bf16_t, 64>(a, plan, st);
-        if (dh == 128) return launch_attend<bf16_t, 128>(a, plan, st);
-        return launch_attend<bf16_t, 256>(a, plan, st);
+        if (dh == 32) return launch_join<bf16_t, 32>(a, plan, st);
+        if (dh == 64) return launch_join<bf16_t, 64>(a, plan, st);
+        if (dh == 128) return launch_join<bf16_t, 128>(a, plan, st);
+        return launch_join<bf16_t, 256>(a, plan, st);
     }
-    if (dh == 32) return launch_attend<float, 32>(a, plan, st);
-    if (dh == 64) return launch_attend<float, 64>(a, plan, st);
-    return launch_attend<float, 128>(a, plan, st);
+    if (dh == 32) return launch_join<float, 32>(a, plan, st);
+    if (dh == 64) return launch_join<float, 64>(a, plan, st);
+    return launch_join<float, 128>(a, plan, st);
 }
 
 }  // namespace metok
@@ -286,8 +296,9 @@ extern "C" int metok_decode_attention(const void* q, int B, int Hq, int Hkv, int
     clear_error();
     if (const char* why = bad_shape(B, Hq, Hkv, S_cap, dh, dtype)) return fail(METOK_ERR_INVALID_ARG, "%s", why);
     const size_t bytes = static_cast<size_t>(B) * Hkv * S_cap * dh * dtype_size(dtype);
-    return attend_impl(q, B, Hq, Hkv, dh, dtype, k_cache, v_cache, S_cap, bytes, nullptr, 0, 1, 0, len, k_new, v_new, scale, logit_cap,
-                       out, lse, weight, weight_stride, workspace, workspace_bytes, stream);
+    return attend_call({q, B, Hq, Hkv, dh, dtype, k_cache, v_cache, S_cap, bytes, nullptr, 0, 1, 0, len, k_new, v_new, scale, logit_cap,
+                        out, lse, weight, weight_stride, workspace, workspace_bytes, stream},
+                       plan_attend(B, Hq, Hkv, S_cap, dh, static_cast<int>(dtype_size(dtype)), weight != nullptr), &launch_decode);
 }
 
 extern "C" int metok_decode_attention_paged(const void* q, int B, int Hq, int Hkv, int dh, int dtype,
@@ -303,6 +314,7 @@ extern "C" int metok_decode_attention_paged(const void* q, int B, int Hq, int Hk
     if (const char* why = bad_shape(B, Hq, Hkv, S_cap, dh, dtype)) return fail(METOK_ERR_INVALID_ARG, "%s", why);
     if (n_pages_pool > INT32_MAX / page_size / Hkv) return fail(METOK_ERR_UNSUPPORTED, "n_pages_pool * Hkv * page_size must be below 2^31");
     const size_t bytes = static_cast<size_t>(n_pages_pool) * Hkv * page_size * dh * dtype_size(dtype);
-    return attend_impl(q, B, Hq, Hkv, dh, dtype, k_pool, v_pool, S_cap, bytes, page_table, n_pages_pool, page_size, pages_per_seq, len,
-                       k_new, v_new, scale, logit_cap, out, lse, weight, weight_stride, workspace, workspace_bytes, stream);
+    return attend_call({q, B, Hq, Hkv, dh, dtype, k_pool, v_pool, S_cap, bytes, page_table, n_pages_pool, page_size, pages_per_seq, len, k_new, v_new, scale, logit_cap,
+                        out, lse, weight, weight_stride, workspace, workspace_bytes, stream},
+                       plan_attend(B, Hq, Hkv, S_cap, dh, static_cast<int>(dtype_size(dtype)), weight != nullptr), &launch_decode);
 }

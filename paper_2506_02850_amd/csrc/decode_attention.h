@@ -602,6 +602,21 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), NB
     }
 }
 
+// What a call of metok_decode_attention, of metok_kv4_attention and of their paged forms goes through behind its own checks: the arguments, and the kernel that
+// reads the cache.  cache_bytes: of K, and of V.
+struct AttendCall {
+    const void* q; int B, Hq, Hkv, dh, dtype;
+    void *k, *v; int64_t S_cap; size_t cache_bytes;
+    const int32_t* table; int64_t n_pages; int page_size, pages_per_seq;
+    const int32_t* len;
+    const void *k_new, *v_new; double scale, logit_cap;
+    void* out; float *lse, *weight; int64_t weight_stride;
+    void* workspace; size_t workspace_bytes; void* stream;
+};
+int attend_call(const AttendCall& c, const AttendPlan& plan, int (*launch)(const DecodeArgs& a, const AttendPlan& plan, int dtype, int dh, hipStream_t st));
+// The limits that they share but the heads', the capacity's and the rows'.
+const char* bad_attend_heads(int B, int Hq, int Hkv, int dh, int dtype);
+
 template <typename T, int DH, int FORM, bool STREAM, int NB>
 void launch_attention(const DecodeArgs& a, unsigned groups, hipStream_t st) {
     if (a.weight) hipLaunchKernelGGL((decode_attention_kernel<T, DH, FORM, true, STREAM, NB>), dim3(groups), dim3(kAttendThreads), 0, st, a);

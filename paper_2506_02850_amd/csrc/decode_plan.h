@@ -60,24 +60,29 @@ struct AttendPlan {
                            // (lse2: a head's maximum and 1 / sum, what the logarithm of its sum is made of)
 };
 
+// What the split goes by beside the shapes: cache rows of a tile, workgroups of a large call, blocks of 16 query heads that a wave takes at a time where a
+// kv head has more than one, and up to how many tiles a pair is left to one workgroup.
+struct AttendSplit { int tile, groups, blocks, whole; };
+
 // `capacity` rows at most, one more with a new row.
-constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int dh, int esize, bool with_weight) {
+constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh, const AttendSplit& split, bool with_weight) {
     AttendPlan p{};
     const int group = Hq / Hkv;
-    p.tile = attend_tile(esize, dh);
+    p.tile = split.tile;
     p.wide = group > kAttendRows;
-    p.block_rows = kAttendRows * (p.wide ? attend_blocks(dh, group) : 1);
+    p.block_rows = kAttendRows * (p.wide ? split.blocks : 1);
     p.row_blocks = (group + p.block_rows - 1) / p.block_rows;
     p.rows = group < p.block_rows ? group : p.block_rows;
     p.pairs = static_cast<int64_t>(B) * Hkv * p.row_blocks;
     const int64_t most = (capacity + 1 + p.tile - 1) / p.tile;                       // tiles of the longest video
-    p.whole = !p.wide && !with_weight && most <= kAttendWhole;
+    p.whole = !p.wide && !with_weight && most <= split.whole;
     p.joined = most > 1 && !p.whole;
-    const int groups = attend_groups(esize, dh);
+    const int groups = split.groups;
     const int64_t few = ((most + kAttendPairCost) * p.pairs + kAttendMinTiles - 1) / kAttendMinTiles;      // workers, with a workgroup each
     p.grid = few < groups ? few : groups;
     p.workers = static_cast<int64_t>(groups) * kAttendWaves;
-    p.logit_stride = with_weight ? (capacity + 1 + 31) / 32 * 32 : 0;
+    const int rounded = p.tile > 32 ? p.tile : 32;                                   // whole tiles are written
+    p.logit_stride = with_weight ? (capacity + 1 + rounded - 1) / rounded * rounded : 0;
     size_t at = 0;
     auto take = [&at](size_t floats) {
         const size_t here = at;
@@ -94,6 +99,16 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     p.logits = take(static_cast<size_t>(B) * Hq * static_cast<size_t>(p.logit_stride));
     p.bytes = at;
     return p;
+}
+constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int dh, int esize, bool with_weight) {
+    return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole}, with_weight);
+}
+
+// The same over a cache in 4 bits (kv4_attention.hip): a row has a quarter of the bytes, so a tile has more of them, and there are two waves to a SIMD.
+constexpr int attend4_tile(int dh) { return dh <= 128 ? 64 : 32; }
+constexpr int kAttend4Groups = 512, kAttend4Whole = 16;
+constexpr AttendPlan plan_attend4(int B, int Hq, int Hkv, int64_t capacity, int dh, bool with_weight) {
+    return plan_split(B, Hq, Hkv, capacity, dh, {attend4_tile(dh), kAttend4Groups, 1, kAttend4Whole}, with_weight);
 }
 
 }  // namespace metok
