@@ -1065,6 +1065,9 @@ def metok_rotate_qk(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos: torc
     given and rotated by the positions pos [axes, B, n] int32 (or [B, n]), pair p of a head's first 2 * len(inv_freq) elements by pos[pair_axis[p]] *
     inv_freq[p]; k and v become rows start[b] + i of the cache [B, Hkv, S_cap, dh].  count [B]: tokens that video b has.  Returns q [B, Hq, n, dh]
     (of tokens that are not there: whatever the tensor held); `out` may carry it."""
+    res = _host.rotate_qk(q, k, v, pos, inv_freq, k_cache, v_cache, None, start, count, pair_axis, q_weight, k_weight, eps, pairs, out, _stream_on)
+    if res is not None:
+        return _native(res)
     return _rotate_qk(q, k, v, pos, inv_freq, k_cache, v_cache, None, start, count, pair_axis, q_weight, k_weight, eps, pairs, out)
 
 
@@ -1075,6 +1078,9 @@ def metok_rotate_qk_paged(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pos
     """metok_rotate_qk into one layer's pools [n_pages, Hkv, page_size, dh] through page_table [B, pages_per_seq]."""
     if page_table is None:
         raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    res = _host.rotate_qk(q, k, v, pos, inv_freq, k_pool, v_pool, page_table, start, count, pair_axis, q_weight, k_weight, eps, pairs, out, _stream_on)
+    if res is not None:
+        return _native(res)
     return _rotate_qk(q, k, v, pos, inv_freq, k_pool, v_pool, page_table, start, count, pair_axis, q_weight, k_weight, eps, pairs, out)
 
 
@@ -1102,6 +1108,9 @@ def _cache4(k: torch.Tensor, v: torch.Tensor, slabs: Optional[int], Hkv: Optiona
 
 
 def _kv4_pack(k, v, k4, v4, page_table, start, count, idx) -> None:
+    res = _host.kv4_pack(k, v, k4, v4, page_table, start, count, idx, _stream_on)
+    if res is not None:
+        return _check(res)
     if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k and v must be of one 4-dimensional shape and type")
     B, Hkv, S_src, dh = (int(x) for x in k.shape)
@@ -1138,6 +1147,9 @@ def metok_kv4_pack_paged(k: torch.Tensor, v: torch.Tensor, k_pool: torch.Tensor,
 
 
 def _kv4_unpack(k4, v4, page_table, lens, n, first, idx, dtype, out) -> Dict[str, torch.Tensor]:
+    res = _host.kv4_unpack(k4, v4, page_table, lens, n, first, idx, out, _stream_on)
+    if res is not None:
+        return _native(res)
     B = int(lens.shape[0]) if lens.dim() == 1 else -1
     kp, vp, slabs, Hkv, rows, dh = _cache4(k4, v4, B if page_table is None else None, None, None)
     if idx is not None:
@@ -1185,6 +1197,9 @@ def metok_kv4_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.T
                         workspace: Optional[torch.Tensor] = None, out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
     """metok_decode_attention over a 4-bit cache (metok_kv4_cache).  k_new / v_new [B, Hkv, dh], of q's type, are put into 4 bits, stored at row lens[b]
     and attended to as what is stored."""
+    res = _host.kv4_attention(q, k_cache, v_cache, None, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, _stream_on)
+    if res is not None:
+        return _native(res)
     return _decode_attention(q, k_cache, v_cache, None, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, four=True)
 
 
@@ -1195,6 +1210,9 @@ def metok_kv4_attention_paged(q: torch.Tensor, k_pool: torch.Tensor, v_pool: tor
     """metok_kv4_attention over 4-bit pools through page_table [B, pages_per_seq]."""
     if page_table is None:
         raise ValueError("page_table must be int32 [B, pages_per_seq]")
+    res = _host.kv4_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, _stream_on)
+    if res is not None:
+        return _native(res)
     return _decode_attention(q, k_pool, v_pool, page_table, lens, k_new, v_new, scale, logit_cap, weight, workspace, out, four=True)
 
 

@@ -21,6 +21,7 @@
 
 #include "metok.h"
 #include "metok_decode.h"
+#include "metok_qkv.h"
 
 namespace {
 
@@ -480,17 +481,20 @@ inline const at::Tensor& fitting(PyObject* o, at::ScalarType type, at::IntArrayR
 }
 inline const at::Tensor& beside(const at::Tensor& t, const at::Tensor& like) { need(t.device() == like.device()); return t; }
 
-// q, k, v, page_table (None: dense), lens, k_new, v_new, scale, logit_cap, weight, workspace, out, stream
+// q, k, v, page_table (None: dense), lens, k_new, v_new, scale, logit_cap, weight, workspace, out, stream; FOUR: over a cache in 4 bits
+template <bool FOUR>
 PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 13, [&](Launch& launch) -> PyObject* {
         const at::Tensor &q = tensor(a[0]), &k = tensor(a[1]);
         need(q.dim() == 3 && k.dim() == 4);
         const auto type = q.scalar_type();
         const int dt = dtype_code(q);
-        const int64_t B = q.size(0), Hq = q.size(1), dh = q.size(2), Hkv = k.size(1), rows = k.size(2);
-        need(B <= INT32_MAX && Hq <= INT32_MAX && dh <= INT32_MAX && Hkv <= INT32_MAX && rows < INT32_MAX);
-        need(k.scalar_type() == type && k.size(3) == dh && k.device() == q.device());
-        const at::Tensor& v = fitting(a[2], type, k.sizes(), q);
+        const auto held = FOUR ? at::kByte : type;
+        const int64_t B = q.size(0), Hq = q.size(1), dh = q.size(2), Hkv = k.size(1);
+        need(B <= INT32_MAX && Hq <= INT32_MAX && dh <= INT32_MAX && Hkv <= INT32_MAX && k.size(2) < INT32_MAX / (FOUR ? 16 : 1));
+        const int64_t rows = k.size(2) * (FOUR ? 16 : 1);
+        need(k.scalar_type() == held && k.size(3) == (FOUR ? 17 * dh / 2 : dh) && k.device() == q.device());
+        const at::Tensor& v = fitting(a[2], held, k.sizes(), q);
         const bool paged = given(a[3]);
         at::Tensor table;
         int64_t cap = rows;
@@ -516,7 +520,7 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const Outputs out(a[11], q);
         const at::Tensor result = beside(out.get("out", {B, Hq, dh}, type), q), lse = beside(out.get("lse", {B, Hq}, at::kFloat), q);
-        const at::Tensor ws = beside(workspace_of(a[10], out, given(a[10]) ? 0 : metok_decode_attention_workspace_bytes(
+        const at::Tensor ws = beside(workspace_of(a[10], out, given(a[10]) ? 0 : (FOUR ? metok_kv4_attention_workspace_bytes : metok_decode_attention_workspace_bytes)(
             static_cast<int>(B), static_cast<int>(Hq), static_cast<int>(Hkv), cap, static_cast<int>(dh), dt, weight.defined())), q);
         Result r;
         r.put("out", result); r.put("lse", lse);
@@ -528,9 +532,162 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
                          static_cast<const int32_t*>(address(lens)), k_new, v_new, scale, logit_cap, address(result), static_cast<float*>(address(lse)), w, w_stride,
                          address(ws), static_cast<size_t>(ws.nbytes()), stream);
         };
-        return answer(paged ? launch(call(&metok_decode_attention_paged, k.size(0), static_cast<int>(rows), static_cast<const int32_t*>(address(table)),
+        return answer(paged ? launch(call(FOUR ? &metok_kv4_attention_paged : &metok_decode_attention_paged, k.size(0), static_cast<int>(rows), static_cast<const int32_t*>(address(table)),
                                           static_cast<int>(table.size(1))))
-                            : launch(call(&metok_decode_attention, rows)), r);
+                            : launch(call(FOUR ? &metok_kv4_attention : &metok_decode_attention, rows)), r);
+    });
+}
+
+// ---- queries, keys and values of new tokens ----------------------------------------------------------------------------
+// An int32 per video, or NULL.
+inline const int32_t* per_video(PyObject* o, int64_t B, const at::Tensor& like) {
+    return given(o) ? static_cast<const int32_t*>(address(fitting(o, at::kInt, {B}, like))) : nullptr;
+}
+// The page table of a paged call.
+struct Table {
+    const int32_t* p = nullptr;
+    int per_seq = 0;
+    Table(PyObject* o, int64_t B, const at::Tensor& like) {
+        if (!given(o)) return;
+        const at::Tensor& t = beside(tensor(o), like);
+        need(t.scalar_type() == at::kInt && t.dim() == 2 && t.size(0) == B && t.size(1) <= INT32_MAX);
+        p = static_cast<const int32_t*>(address(t));
+        per_seq = static_cast<int>(t.size(1));
+    }
+};
+// Rows of tokens [B, n, heads, dh] that may be parts of a wider buffer: elements between tokens.
+struct TokenRows {
+    void* p;
+    int heads;
+    int64_t stride;
+    TokenRows(PyObject* o, const at::Tensor& like) {
+        need(THPVariable_CheckExact(o));
+        const at::Tensor& t = THPVariable_Unpack(o);
+        need(t.is_cuda() && t.layout() == at::kStrided && t.dim() == 4 && t.scalar_type() == like.scalar_type() && t.device() == like.device() &&
+             t.size(0) == like.size(0) && t.size(1) == like.size(1) && t.size(3) == like.size(3) && t.size(2) <= INT32_MAX && t.numel() > 0);
+        const int64_t B = t.size(0), n = t.size(1), dh = t.size(3);
+        heads = static_cast<int>(t.size(2));
+        stride = n > 1 ? t.stride(1) : B > 1 ? t.stride(0) : heads * dh;
+        need((t.stride(3) == 1) && (heads == 1 || t.stride(2) == dh) && (B == 1 || t.stride(0) == n * stride));
+        p = address(t);
+    }
+};
+
+// q, k, v, pos, inv_freq, k_cache, v_cache, page_table (None: dense), start, count, pair_axis, q_weight, k_weight, eps, pairs, out, stream
+PyObject* rotate_qk(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded(n_args, 17, [&](Launch& launch) -> PyObject* {
+        need(THPVariable_CheckExact(a[0]));
+        const at::Tensor& like = THPVariable_Unpack(a[0]);
+        need(like.is_cuda() && like.dim() == 4 && like.size(0) <= INT32_MAX && like.size(3) <= INT32_MAX);
+        const auto type = like.scalar_type();
+        const int dt = dtype_code(like);
+        const int64_t B = like.size(0), n = like.size(1), dh = like.size(3);
+        const TokenRows q(a[0], like), k(a[1], like), v(a[2], like);
+        need(k.heads == v.heads);
+        const at::Tensor& k_to = beside(tensor(a[5]), like);
+        need(k_to.dim() == 4 && k_to.scalar_type() == type && k_to.size(1) == k.heads && k_to.size(3) == dh && k_to.size(2) <= INT32_MAX);
+        const at::Tensor& v_to = fitting(a[6], type, k_to.sizes(), like);
+        const Table table(a[7], B, like);
+        need(table.p || k_to.size(0) == B);
+        const at::Tensor &pos = beside(tensor(a[3]), like), &freq = beside(tensor(a[4]), like);
+        need(pos.scalar_type() == at::kInt && (pos.dim() == 3 || pos.dim() == 2) && pos.size(-2) == B && pos.size(-1) == n && freq.scalar_type() == at::kFloat && freq.dim() == 1);
+        const int64_t axes = pos.dim() == 3 ? pos.size(0) : 1, half = freq.size(0);
+        need(axes <= INT32_MAX && half <= 1024);
+        const uint8_t* axis = nullptr;
+        if (given(a[10])) {
+            need(PyBytes_CheckExact(a[10]) && PyBytes_GET_SIZE(a[10]) == half);
+            axis = reinterpret_cast<const uint8_t*>(PyBytes_AS_STRING(a[10]));
+        }
+        auto weight = [&](PyObject* o) { return given(o) ? address(fitting(o, type, {dh}, like)) : nullptr; };
+        void *q_weight = weight(a[11]), *k_weight = weight(a[12]);
+        const double eps = real(a[13]);
+        const int pairs = int32(a[14]);
+        const int32_t *start = per_video(a[8], B, like), *count = per_video(a[9], B, like);
+        const Outputs out(a[15], like);
+        const at::Tensor to = beside(out.get("q", {B, q.heads, n, dh}, type), like);
+        Result r;
+        r.put("q", to);
+        void* stream = stream_on(a[16], like);
+        auto call = [&](auto f, auto... tail) {
+            return bound(f, q.p, k.p, v.p, q.stride, k.stride, v.stride, static_cast<int>(B), n, q.heads, k.heads, static_cast<int>(dh), dt, count, q_weight, k_weight, eps,
+                         static_cast<const int32_t*>(address(pos)), static_cast<int>(axes), static_cast<const float*>(address(freq)), axis, static_cast<int>(2 * half), pairs,
+                         address(to), address(k_to), address(v_to), tail..., start, stream);
+        };
+        return answer(table.p ? launch(call(&metok_rotate_qk_paged, k_to.size(0), static_cast<int>(k_to.size(2)), table.p, table.per_seq))
+                              : launch(call(&metok_rotate_qk, k_to.size(2))), r);
+    });
+}
+
+// A cache in 4 bits or its pools: [slabs, Hkv, rows / 16, 17 dh / 2] bytes.
+struct Cache4 {
+    const at::Tensor &k, &v;
+    int64_t slabs, rows;
+    int Hkv, dh;
+    Cache4(PyObject* ko, PyObject* vo, const at::Tensor& like) : k(beside(tensor(ko), like)), v(fitting(vo, at::kByte, k.sizes(), like)) {
+        need(k.scalar_type() == at::kByte && k.dim() == 4 && k.size(1) <= INT32_MAX && k.size(2) < INT32_MAX / 16 && k.size(3) <= INT32_MAX / 2);
+        slabs = k.size(0);
+        Hkv = static_cast<int>(k.size(1));
+        rows = 16 * k.size(2);
+        dh = static_cast<int>(k.size(3) * 2 / 17);
+        need(17 * dh / 2 == k.size(3));
+    }
+};
+
+// k, v, k_cache, v_cache, page_table (None: dense), start, count, idx, stream
+PyObject* kv4_pack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded(n_args, 9, [&](Launch& launch) -> PyObject* {
+        const at::Tensor& k = tensor(a[0]);
+        const int dt = dtype_code(k);
+        need(k.dim() == 4 && k.size(0) <= INT32_MAX);
+        const at::Tensor& v = fitting(a[1], k.scalar_type(), k.sizes(), k);
+        const Cache4 to(a[2], a[3], k);
+        const int64_t B = k.size(0);
+        need(to.Hkv == k.size(1) && to.dh == k.size(3));
+        const Table table(a[4], B, k);
+        need(table.p || to.slabs == B);
+        const int32_t *start = per_video(a[5], B, k), *count = per_video(a[6], B, k), *idx = nullptr;
+        int64_t n = k.size(2);
+        if (given(a[7])) {
+            const at::Tensor& t = beside(tensor(a[7]), k);
+            need(t.scalar_type() == at::kInt && t.dim() == 2 && t.size(0) == B);
+            idx = static_cast<const int32_t*>(address(t));
+            n = t.size(1);
+        }
+        Owned done(PyLong_FromLong(METOK_OK));
+        void* stream = stream_on(a[8], k);
+        auto call = [&](auto f, auto... tail) {
+            return bound(f, address(k), address(v), static_cast<int>(B), to.Hkv, k.size(2), to.dh, dt, idx, n, count, address(to.k), address(to.v), tail..., start, stream);
+        };
+        return answer(table.p ? launch(call(&metok_kv4_pack_paged, to.slabs, static_cast<int>(to.rows), table.p, table.per_seq)) : launch(call(&metok_kv4_pack, to.rows)), done);
+    });
+}
+
+// k_cache, v_cache, page_table (None: dense), lens, n, first, idx, out, stream; both outputs are given
+PyObject* kv4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
+    return guarded(n_args, 9, [&](Launch& launch) -> PyObject* {
+        const Cache4 from(a[0], a[1], tensor(a[0]));
+        const at::Tensor& lens = beside(tensor(a[3]), from.k);
+        need(lens.scalar_type() == at::kInt && lens.dim() == 1 && lens.size(0) <= INT32_MAX);
+        const int64_t B = lens.size(0), n = integer(a[4]);
+        const Table table(a[2], B, from.k);
+        need(table.p || from.slabs == B);
+        const Outputs out(a[7], from.k);
+        PyObject *ko = out.find("k"), *vo = out.find("v");
+        need(ko && vo);
+        const at::Tensor& k = beside(tensor(ko), from.k);
+        const int dt = dtype_code(k);
+        need(k.dim() == 4 && k.size(0) == B && k.size(1) == from.Hkv && k.size(3) == from.dh);
+        const at::Tensor& v = fitting(vo, k.scalar_type(), k.sizes(), k);
+        const int32_t *first = per_video(a[5], B, from.k), *idx = given(a[6]) ? static_cast<const int32_t*>(address(fitting(a[6], at::kInt, {B, n}, from.k))) : nullptr;
+        Result r;
+        r.put("k", k); r.put("v", v);
+        void* stream = stream_on(a[8], from.k);
+        auto call = [&](auto f, auto... middle) {
+            return bound(f, address(from.k), address(from.v), static_cast<int>(B), from.Hkv, middle..., static_cast<const int32_t*>(address(lens)), first, idx, n,
+                         address(k), address(v), k.size(2), dt, stream);
+        };
+        return answer(table.p ? launch(call(&metok_kv4_unpack_paged, from.slabs, static_cast<int>(from.rows), from.dh, table.p, table.per_seq))
+                              : launch(call(&metok_kv4_unpack, from.rows, from.dh)), r);
     });
 }
 
@@ -655,7 +812,11 @@ PyMethodDef methods[] = {
     {"prefill_prune_batched", METOK_HOST_CALL(&prefill_prune_batched)},
     {"kv_compact", METOK_HOST_CALL(&kv_compact)},
     {"kv_relink_paged", METOK_HOST_CALL(&kv_relink_paged)},
-    {"decode_attention", METOK_HOST_CALL(&decode_attention)},
+    {"decode_attention", METOK_HOST_CALL(&decode_attention<false>)},
+    {"kv4_attention", METOK_HOST_CALL(&decode_attention<true>)},
+    {"rotate_qk", METOK_HOST_CALL(&rotate_qk)},
+    {"kv4_pack", METOK_HOST_CALL(&kv4_pack)},
+    {"kv4_unpack", METOK_HOST_CALL(&kv4_unpack)},
     {"kv_evict", METOK_HOST_CALL(&kv_evict)},
     {"kv_evict_select", METOK_HOST_CALL(&kv_evict_select)},
     {nullptr, nullptr, 0, nullptr},
