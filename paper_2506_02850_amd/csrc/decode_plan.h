@@ -104,11 +104,11 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole}, with_weight);
 }
 
-// The same over a cache in 4 bits (kv4_attention.hip): a row has a quarter of the bytes, so a tile has more of them, and there are two waves to a SIMD.
-constexpr int attend4_tile(int dh) { return dh <= 128 ? 64 : 32; }
-constexpr int kAttend4Groups = 512, kAttend4Whole = 16;
+// The same over a cache in 4 bits (kv4_attention.hip): a row has a quarter of the bytes, so there are two waves to a SIMD.
+constexpr int kAttend4Tile = 32, kAttend4Groups = 512;
+constexpr int kAttend4Whole = 32;
 constexpr AttendPlan plan_attend4(int B, int Hq, int Hkv, int64_t capacity, int dh, bool with_weight) {
-    return plan_split(B, Hq, Hkv, capacity, dh, {attend4_tile(dh), kAttend4Groups, 1, kAttend4Whole}, with_weight);
+    return plan_split(B, Hq, Hkv, capacity, dh, {kAttend4Tile, kAttend4Groups, 1, kAttend4Whole}, with_weight);
 }
 
 }  // namespace metok

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     static_assert(!WHOLE || !WEIGHTS, "the second launch adds the weights up");
     using F = Block4<DH>;
     constexpr bool BF16 = sizeof(T) == 2;
-    constexpr int TILE = attend4_tile(DH), NT = TILE / 16, NV = NT * 4, P = F::kPieces, KW = F::kWidth / 32, EB = F::kRunBytes, E = DH / 16, RB = DH * static_cast<int>(sizeof(T));
+    constexpr int TILE = kAttend4Tile, NT = TILE / 16, NV = NT * 4, P = F::kPieces, KW = F::kWidth / 32, EB = F::kRunBytes, E = DH / 16, RB = DH * static_cast<int>(sizeof(T));
     constexpr int QP = BF16 ? 1 : 3, PP = BF16 ? 2 : 3;    // parts of a query, of a probability
     static_assert(NT % 2 == 0 && KW == EB, "32 rows to a product; a lane has as much of K as of V");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
@@ -85,6 +85,13 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     auto n_heads = [&](const Cursor& x) { return min(a.group - x.rb * kAttendRows, kAttendRows); };
     auto slab_of = [&](const Cursor& x) { return static_cast<int64_t>(x.b) * a.Hkv + x.kvh; };
 
+    // What depends on the lane is kept from the compiler's sight where it is used.  In the loads it stays the 32-bit offset beside a block's address in scalar
+    // registers; elsewhere it is computed when it is needed.  Hoisted out of the loop, as addresses of 64 bits, all that takes 40 registers and an
+    // addition a load.
+    auto hidden = [](uint32_t x) { asm("" : "+v"(x)); return x; };
+    struct Lane { int lane, r, c; };
+    auto lane_here = [&] { const int x = static_cast<int>(hidden(lane)); return Lane{x, x & 15, x >> 4}; };
+
     // ---- loads ----
     auto page_index = [&](int j) { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(j)) * a.page_mul) >> a.page_shift); };
     struct Pages { int p[PAGED ? NT : 1]; };               // table entries of a tile's blocks
@@ -99,7 +106,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         return p;
     };
     // The tile's blocks in the slab or pool (behind the last row: the block with the last row, where there is none the first one), and which of them are there.
-    struct Rows { int block[NT]; bool all; uint32_t pages_ok; };       // all: the tile ends before the last row, and its pages are ones
+    struct Rows { int block[NT], all; uint32_t pages_ok; };            // all: the tile ends before the last row, and its pages are ones
     auto rows_of = [&](const Cursor& x, const Pages& p) {
         Rows f{};
         const int j0 = x.t * TILE, last = max(x.n - 1, 0);
@@ -112,7 +119,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             if constexpr (PAGED) {
                 const bool ok = p.p[b] >= 0 && p.p[b] < a.n_pages;
                 f.block[b] = ok ? (p.p[b] * a.Hkv + x.kvh) * (a.page_size / kBlockRows) + (j - page_index(j) * a.page_size) / kBlockRows : 0;
-                if (!ok) { f.pages_ok &= ~(1u << b); f.all = false; }
+                if (!ok) { f.pages_ok &= ~(1u << b); f.all = 0; }
             }
         }
         return f;
@@ -124,30 +131,33 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         return cache + ((PAGED ? 0 : slab_of(x) * (a.S_cap / kBlockRows)) + block) * F::kBytes;
     };
     auto load_k = [&](const Cursor& x, const Rows& f) {
+        const uint32_t code = hidden(k_code), scale = hidden(k_scale);
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
             const char* block = base_of(x, a.k, f.block[b]);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                load_words<KW, STREAM>(kf[b][p], block + p * F::kPieceBytes + k_code);
-                ks[b][p] = *reinterpret_cast<const uint8_t*>(block + p * 16 * F::kGroups + k_scale);
+                load_words<KW, STREAM>(kf[b][p], block + p * F::kPieceBytes + code);
+                ks[b][p] = *reinterpret_cast<const uint8_t*>(block + p * 16 * F::kGroups + scale);
             }
         }
     };
     auto load_v = [&](const Cursor& x, const Rows& f) {
+        const uint32_t code = hidden(v_code), scale = hidden(v_scale);
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
             const char* block = base_of(x, a.v, f.block[b]);
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                load_words<KW, STREAM>(vf[b][p], block + p * F::kPieceBytes + v_code);
-                vs[b][p] = *reinterpret_cast<const uint32_t*>(block + p * 16 * F::kGroups + v_scale);
+                load_words<KW, STREAM>(vf[b][p], block + p * F::kPieceBytes + code);
+                vs[b][p] = *reinterpret_cast<const uint32_t*>(block + p * 16 * F::kGroups + scale);
             }
         }
     };
     // queries in the order of the codes: word i of piece p of the lane's part of a row of K is elements p w + c w / 4 + 8 i ..
     u32x4_t qf[P * KW][QP];
     auto load_q = [&](const Cursor& x) {
+        const auto [lane, r, c] = lane_here();
         const char* head = a.q + (static_cast<int64_t>(x.b) * a.Hq + first_head(x) + min(r, n_heads(x) - 1)) * RB;
 #pragma unroll
         for (int i = 0; i < P * KW; ++i) {
@@ -171,6 +181,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     auto new_row = [&](const Cursor& x) { return fresh && static_cast<int>(static_cast<uint32_t>(x.n) / TILE) == x.t; };
     // two elements to a lane, 128 at a time; heads of fewer have lanes that do the same
     auto pack_new = [&](const Cursor& x) {
+        const auto [lane, r, c] = lane_here();
 #pragma unroll
         for (int which = 0; which < 2; ++which)
 #pragma unroll
@@ -188,6 +199,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         __builtin_amdgcn_wave_barrier();
     };
     auto place_new = [&](const Cursor& x) {
+        const auto [lane, r, c] = lane_here();
         const int in = x.n - x.t * TILE;                   // the new row's place in the tile
         const uint8_t *nk = s_new[wave][0], *nv = s_new[wave][1];
 #pragma unroll
@@ -220,6 +232,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     // it joins the cache: nobody uses what the cache has in that row in this call
     auto append = [&](const Cursor& x) {
         if (!new_row(x) || x.rb != 0 || x.n >= a.S_cap) return;
+        const auto [lane, r, c] = lane_here();
         int64_t block = slab_of(x) * (a.S_cap / kBlockRows) + x.n / kBlockRows;
         if constexpr (PAGED) {
             const int index = page_index(x.n), page = a.table[static_cast<int64_t>(x.b) * a.pages_per_seq + index];
@@ -280,6 +293,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         }
         const float scale = score_scale(a);
         if (!f.all) {
+            const auto [lane, r, c] = lane_here();
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int j = x.t * TILE + 16 * (i >> 2) + 4 * c + (i & 3);
@@ -291,6 +305,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             }
         }
         if constexpr (WEIGHTS) {
+            const auto [lane, r, c] = lane_here();
             if (r < n_heads(x)) {
                 float* to = a.logits + (static_cast<int64_t>(x.b) * a.Hq + first_head(x) + r) * a.logit_stride + x.t * TILE + 4 * c;
 #pragma unroll
@@ -360,6 +375,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     // ---- the end of a pair, or of the worker's tiles: the result, or a part of it for the join ----
     constexpr int N = 2 * EB;                              // accumulator i of element e: element (e / N) * w + N (4 c + i) + e % N
     auto finish = [&](const Cursor& x, int begun) {        // begun: the first tile of the pair that the worker had
+        const auto [lane, r, c] = lane_here();
         const bool ends = x.t == x.tiles - 1, whole = begun == 0 && ends;
         if (a.pair_workers && lane == 0) {
             int* to = reinterpret_cast<int*>(a.pair_workers + slab_of(x) * a.row_blocks + x.rb);
@@ -413,34 +429,36 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         int begun = at.t;                                  // first tile of the pair that the worker has
         load_q(at);
         Rows rows = rows_of(at, pages_of(at));
+        __builtin_amdgcn_sched_barrier(0);                 // in the loop's order, or its waits would allow for both
         load_k(at, rows);
+        __builtin_amdgcn_sched_barrier(0);
         load_v(at, rows);
         for (;;) {
             const bool ends = !WHOLE && at.t == at.tiles - 1;
             left -= ends ? 1 + kAttendPairCost : 1;
             const bool last = left <= 0;
-            const Cursor next = last ? at : advance(at);
-            Rows rows_next = rows;
+            // Behind the last tile the first one of all is loaded, for nobody: with loads that may not be there the waits for those before them would wait for
+            // everything (8 x 36992 rows, 28 heads on 4 of 128: 47 us).
+            const Cursor next = last ? Cursor{0, 0, 0, 0, 1, 0} : advance(at);
+            const Pages pages = pages_of(next);
             if (new_row(at)) {
                 pack_new(at);
                 place_new(at);
             }
             f32x4_t s[NT];
             scores(s);
-            if (!last) {
-                rows_next = rows_of(next, pages_of(next));
-                load_k(next, rows_next);
-            }
+            const Rows rows_next = rows_of(next, pages);
+            load_k(next, rows_next);
             take(at, rows, s);
             if (ends || (!WHOLE && last)) finish(at, begun);
             append(at);
-            if (last) break;
-            if (ends) {
+            if (ends && !last) {
                 begun = 0;
                 clear();
                 load_q(next);
             }
             load_v(next, rows_next);
+            if (last) break;
             at = next;
             rows = rows_next;
         }
