@@ -9,6 +9,16 @@
 
 namespace metok {
 
+// The scale in byte I of a word.
+template <int I> __device__ __forceinline__ float scale_in(uint32_t w) {
+    uint32_t x;
+    if constexpr (I == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(x) : "v"(23), "v"(w));
+    else if constexpr (I == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(x) : "v"(23), "v"(w));
+    else if constexpr (I == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(x) : "v"(23), "v"(w));
+    else asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(x) : "v"(23), "v"(w));
+    return __uint_as_float(x);
+}
+
 // x as the sum of PARTS bf16 numbers, 8 bits each: all of a bf16 number's bits in one, of an fp32 number's in three.
 template <int PARTS> __device__ __forceinline__ void split_pair(uint32_t (&part)[PARTS], float a, float b) {
 #pragma unroll
@@ -298,7 +308,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             for (int i = 0; i < NV; ++i) {
                 const int j = x.t * TILE + 16 * (i >> 2) + 4 * c + (i & 3);
                 const bool there = (j < x.n && ((f.pages_ok >> (i >> 2)) & 1u)) || (fresh && j == x.n);
-                if (!there) s[i >> 2][i & 3] = -INFINITY;
+                s[i >> 2][i & 3] = there ? s[i >> 2][i & 3] : -INFINITY;
                 const uint32_t byte = 0xffu << (8 * (i & 3)), one = 127u << (8 * (i & 3));
 #pragma unroll
                 for (int p = 0; p < P; ++p) vs[i >> 2][p] = there ? vs[i >> 2][p] : (vs[i >> 2][p] & ~byte) | one;       // finite: nothing times it is nothing
@@ -315,9 +325,11 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         float top = s[0][0];
 #pragma unroll
         for (int i = 1; i < NV; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-        top = rows_max(top);
-        if (__any(top > m)) {
-            const float to = fmaxf(m, top), g = exp2_from(m, to == -INFINITY ? 0.f : to, scale);
+        // What probabilities are relative to follows the maximum only where that is more than 2^kLag times it: sums and products are fp32 numbers of any
+        // size, and with several heads some maximum grows in most tiles of a short run.
+        constexpr float kLag = 8.f;
+        if (__any((top - m) * scale > kLag)) {
+            const float to = fmaxf(m, rows_max(top)), g = exp2_from(m, to == -INFINITY ? 0.f : to, scale);
             m = to;
             l *= g;
 #pragma unroll
@@ -325,10 +337,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         }
         const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-        for (int h = 0; h < NT / 2; ++h) {                 // 32 rows to a product
+        for (int h = 0; h < NT / 2; ++h) {                 // 32 rows to a product: rows 4 c .. 4 c + 3 of the one block, then of the other
             u32x4_t part[PP];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                  // rows 4 c .. 4 c + 3 of the one block, then of the other
+            for (int i = 0; i < 4; ++i) {
                 const int b = 2 * h + (i >> 1), at0 = 2 * (i & 1);
                 const float p0 = exp2_from(s[b][at0], ref, scale), p1 = exp2_from(s[b][at0 + 1], ref, scale);
                 l += p0;
@@ -342,7 +354,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             for (int p = 0; p < P; ++p) {
                 float vscale[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) vscale[i] = scale_from((vs[2 * h + (i >> 2)][p] >> (8 * (i & 3))) & 0xffu);
+                for (int b = 0; b < 2; ++b) {
+                    const uint32_t w = vs[2 * h + b][p];
+                    vscale[4 * b] = scale_in<0>(w); vscale[4 * b + 1] = scale_in<1>(w); vscale[4 * b + 2] = scale_in<2>(w); vscale[4 * b + 3] = scale_in<3>(w);
+                }
 #pragma unroll
                 for (int z = 0; z < EB; ++z) {
                     uint32_t two[8];                       // elements 2 z, 2 z + 1 of the run, of each of the lane's rows
@@ -371,7 +386,6 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             }
         }
     };
-
     // ---- the end of a pair, or of the worker's tiles: the result, or a part of it for the join ----
     constexpr int N = 2 * EB;                              // accumulator i of element e: element (e / N) * w + N (4 c + i) + e % N
     auto finish = [&](const Cursor& x, int begun) {        // begun: the first tile of the pair that the worker had
