@@ -29,7 +29,7 @@ enum { METOK_PAIRS_HALVES = 0, METOK_PAIRS_ADJACENT = 1 };   /* which elements o
  *                be parts of one buffer, as one product leaves them.
  *   count        device, [B] int32, or NULL (= n): video b has its first count[b] tokens, of the others nothing is read or written.
  *   q_weight, k_weight  device, [dh] of `dtype`, or both NULL (no norm): x_e becomes x_e / sqrt(mean over the head's dh elements of x^2 + eps) *
- *                weight_e.  eps in [0, 1]; a head whose mean square is 0 (in fp32) with eps = 0 becomes zeros.
+ *                weight_e.  eps in [0, 1]; a head whose mean square and eps add up to less than 2^-126 becomes zeros.
  *   pos          device, [n_axes, B, n] int32 (1 <= n_axes <= METOK_MAX_POSITION_AXES): the tokens' positions.
  *   inv_freq     device, [rot / 2] float, finite: pair p is rotated by the angle pos[pair_axis[p]] * inv_freq[p] radians.  The product is not rounded to
  *                fp32, so that far positions keep their angles.
@@ -42,7 +42,7 @@ enum { METOK_PAIRS_HALVES = 0, METOK_PAIRS_ADJACENT = 1 };   /* which elements o
  *                rotated, its values as they are; rows that are not below S_cap are not stored.
  *   start        device, [B] int32, or NULL (= 0).
  *   Norms and rotations are computed in fp32 and rounded once.
- *   Limits: dh in {32, 64, 128, 256} for bf16, {32, 64, 128} for f32; 1 <= B <= METOK_MAX_DECODE_BATCH; 1 <= n and B * n <= 2^27; Hq + 2 Hkv <= 4096; Hq need
+ *   Limits: dh in {32, 64, 128, 256} for bf16, {32, 64, 128} for f32; 1 <= B <= METOK_MAX_DECODE_BATCH; 1 <= n and B * n <= 2^26; Hq + 2 Hkv <= 4096; Hq need
  *   not be a multiple of Hkv; S_cap below 2^31 - 64; a head's sum of squares finite in fp32.  q_out and the caches must not overlap each other or anything that the call reads.
  * ------------------------------------------------------------------------------------------- */
 METOK_API int metok_rotate_qk(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,

@@ -2,18 +2,24 @@
 // position (one to four axes: time, height and width for the tokens of a video), queries laid out head by head, keys and values put into the
 // dense or paged cache.
 //
-// One pass: (Hq + 2 Hkv) dh elements of a token are read and as many written.  HBM bounds a prompt, the launch a step.
+// One pass: (Hq + 2 Hkv) dh elements of a token are read and as many written.  HBM bounds a prompt (18560 tokens of 36 heads of 128 in bf16, 342 MB: 64 us,
+// 5.3 TB/s; a copy in the order of the addresses 53), the launch and its latencies a step.
 #include "common.h"
 #include "metok_qkv.h"
 
 namespace metok {
 
 constexpr int kRotateThreads = 256, kRotateWaves = kRotateThreads / 64;
-constexpr int kLaneElems = 16;                             // elements of a head that a lane has
-constexpr int kMaxHead = 256;
-// Waves that a call is spread over, at most: where it has fewer (token, head) rows, a wave takes one head of its tokens, and the cosines and
-// sines are computed by each of them.
-constexpr int kRotateSpread = 8192;
+constexpr int kRotUnit = 16, kMaxPairs = 128;              // rot is a multiple of; pairs of a head at most
+constexpr int kAtOnce = 4;                                 // heads whose loads are on their way together
+// Heads that a workgroup takes where there are kRotateSpread workgroups of one head or more: enough for the cosines and sines to be a small part of its work, few enough
+// for the writes to stay in order (18560 tokens, 36 heads of 128, bf16: 4 heads 66.5 us, 8 64.4, 12 64.2, 20 73; 11000 of 18 of 64, fp32: 4 20.6, 8 22.1, 12 21.6;
+// without any arithmetic 62).  A step of 64 tokens, 36 heads: 5.1 us, which is launch, positions, sine and product one behind the other.
+constexpr int rotate_heads(int esize) { return 16 / esize; }
+constexpr int kRotateSpread = 4096;
+// Rows of more bytes than this are read, or written, with the streaming hint: the prompt above 64 us with both, 68 without that on the reads; the fp32 one, whose rows the
+// memory-side cache still holds, 24 with it on the writes, 31 without, 33 on both.
+constexpr int64_t kStreamIn = 128 << 20, kStreamOut = 32 << 20;
 
 struct RotateArgs {
     const char *q, *k, *v;
@@ -23,16 +29,16 @@ struct RotateArgs {
     const float* inv_freq;
     int64_t q_stride, k_stride, v_stride;                  // bytes between tokens
     int64_t n, tokens;                                     // of a video, of all
-    int B, Hq, Hkv, S_cap, n_axes, rot, per_wave;          // per_wave: heads that a wave takes
+    int B, Hq, Hkv, S_cap, n_axes, rot, per_group;         // per_group: heads that a workgroup takes
     int page_size, pages_per_seq, n_pages;
     float eps;
-    uint64_t axis[kMaxHead / kLaneElems];                  // a byte per pair
+    uint8_t axis[kMaxPairs];
 };
 
-// Eight neighbouring elements.
-template <typename T> struct Chunk8;
-template <> struct Chunk8<bf16_t> {
-    typedef uint4 type;
+// 16 bytes of neighbouring elements, a run.
+template <typename T> struct Run;
+template <> struct Run<bf16_t> {
+    static constexpr int kElems = 8;
     static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
         x[0] = bf16_lo(v.x); x[1] = bf16_hi(v.x); x[2] = bf16_lo(v.y); x[3] = bf16_hi(v.y);
         x[4] = bf16_lo(v.z); x[5] = bf16_hi(v.z); x[6] = bf16_lo(v.w); x[7] = bf16_hi(v.w);
@@ -41,15 +47,27 @@ template <> struct Chunk8<bf16_t> {
         return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
     }
 };
-template <> struct Chunk8<float> {
-    struct type { float4 a, b; };
-    static __device__ __forceinline__ void unpack(const type& v, float (&x)[8]) {
-        x[0] = v.a.x; x[1] = v.a.y; x[2] = v.a.z; x[3] = v.a.w; x[4] = v.b.x; x[5] = v.b.y; x[6] = v.b.z; x[7] = v.b.w;
+template <> struct Run<float> {
+    static constexpr int kElems = 4;
+    static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
+        x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
     }
-    static __device__ __forceinline__ type pack(const float (&x)[8]) {
-        return {make_float4(x[0], x[1], x[2], x[3]), make_float4(x[4], x[5], x[6], x[7])};
+    static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
     }
 };
+
+// Sum over LANES neighbouring lanes (4 .. 32); each receives it.
+template <int CTRL> __device__ __forceinline__ float dpp_sum(float v) {
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, false));
+}
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) {
+    v = dpp_sum<0xb1>(v);                                  // the neighbour
+    v = dpp_sum<0x4e>(v);                                  // two further, within four
+    if (LANES >= 8) v = dpp_sum<0x141>(v);                 // mirrored within eight: the other four
+    if (LANES >= 16) v = dpp_sum<0x140>(v);                // mirrored within sixteen
+    return LANES == 32 ? swap16_add(v, v) : v;
+}
 
 // Cosine and sine of pos * freq.  In revolutions, in 64 bits, of which the whole ones are taken off: an fp32 product is off by 2^-24 of itself, 0.006
 // radians at a position of 100000.
@@ -59,43 +77,37 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float& cos, float& 
     sincospif(2.f * static_cast<float>(x - rint(x)), &sin, &cos);
 }
 
-// A lane has 16 elements of a head of a token, as two runs of 8: rotated halves p .. p + 7 and rot / 2 + p .. of 8 pairs (16 neighbouring elements where the
-// pairs are adjacent or not rotated).  It keeps its token and its pairs, and with them the cosines and sines, through the heads that the wave takes.
-template <typename T, int DH, bool ADJACENT>
+// A lane has a run of a head of a token, the lanes of a wave the rows of neighbouring tokens, and a workgroup so many tokens of a few heads.  Workgroups with
+// neighbouring tokens follow each other, those of the next heads come behind all of them: what is written is written in the order of its addresses, 256
+// bytes and more at a time, and it is the reads that jump (18560 tokens of 36 heads of 128 in bf16, copied alone: 56 us so, 61 to 71 with the reads in order, 66
+// with a head's halves in two stores; a plain copy 53).
+//
+// The other half of a pair is with another lane.  With c, s the pair's cosine and sine, g and g' the weights of the lane's element x and of the other one x', and
+// f = 1 / root mean square, the result is f (x (g c) +- x' (g' s)): two factors to an element, computed once for all heads of a kind.
+template <typename T, int DH, bool ADJACENT, bool STREAM_IN, bool STREAM_OUT>
 __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(const RotateArgs a) {
-    constexpr int LANES = DH / kLaneElems, TOKENS = 64 / LANES, ES = sizeof(T);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), x = lane % LANES;
-    const int64_t token = (static_cast<int64_t>(blockIdx.x) * kRotateWaves + wave) * TOKENS + lane / LANES;
-    const int64_t at = min(token, a.tokens - 1);
-    const int b = static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(a.n)), i = static_cast<int>(at - b * a.n);
-    const bool here = token < a.tokens && (!a.count || i < a.count[b]);
-    const int heads = a.Hq + 2 * a.Hkv, h0 = blockIdx.y * a.per_wave, h1 = min(h0 + a.per_wave, heads);
-    if (!__any(here)) return;
+    constexpr int R = Run<T>::kElems, LANES = DH / R, TOKENS = kRotateThreads / LANES, ES = sizeof(T), PAIRS = DH / 2;
+    const int x = threadIdx.x % LANES, mine = threadIdx.x / LANES;
+    const int64_t token0 = static_cast<int64_t>(blockIdx.x) * TOKENS, at = min(token0 + mine, a.tokens - 1);
+    const int b = static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(a.n)), i = static_cast<int>(at - static_cast<int64_t>(b) * a.n);
+    const bool here = token0 + mine < a.tokens && (!a.count || i < a.count[b]);
+    const int turned_heads = a.Hq + a.Hkv, heads = turned_heads + a.Hkv, h0 = blockIdx.y * a.per_group, h1 = min(h0 + a.per_group, heads);
 
-    const bool turned = x * kLaneElems < a.rot;
-    const int e0 = ADJACENT || !turned ? x * kLaneElems : x * 8, e1 = ADJACENT || !turned ? e0 + 8 : a.rot / 2 + x * 8;
-    float cos[8], sin[8];
-    if (turned && h0 < a.Hq + a.Hkv) {
-        int pos[METOK_MAX_POSITION_AXES];
+    // the cosines and sines of the workgroup's tokens, pair by pair over its threads
+    __shared__ float s_cos[TOKENS * PAIRS], s_sin[TOKENS * PAIRS];
+    if (h0 < turned_heads) {
 #pragma unroll
-        for (int d = 0; d < METOK_MAX_POSITION_AXES; ++d) pos[d] = d < a.n_axes ? a.pos[d * a.tokens + at] : 0;
-        const uint64_t axis = a.axis[x];
-        const float4 f0 = *reinterpret_cast<const float4*>(a.inv_freq + 8 * x), f1 = *reinterpret_cast<const float4*>(a.inv_freq + 8 * x + 4);
-        const float freq[8] = {f0.x, f0.y, f0.z, f0.w, f1.x, f1.y, f1.z, f1.w};
-#pragma unroll
-        for (int p = 0; p < 8; ++p) {
-            const int d = static_cast<int>(axis >> (8 * p)) & 3;
-            turn_of(d < 2 ? (d == 0 ? pos[0] : pos[1]) : (d == 2 ? pos[2] : pos[3]), freq[p], cos[p], sin[p]);
+        for (int k = 0; k < TOKENS * PAIRS / kRotateThreads; ++k) {
+            const int place = threadIdx.x + k * kRotateThreads, pair = place % PAIRS;
+            const int64_t of = min(token0 + place / PAIRS, a.tokens - 1);
+            if (pair < a.rot / 2) turn_of(a.pos[a.axis[pair] * a.tokens + of], a.inv_freq[pair], s_cos[place], s_sin[place]);
         }
-    } else {
-#pragma unroll
-        for (int p = 0; p < 8; ++p) { cos[p] = 1.f; sin[p] = 0.f; }
     }
+    __syncthreads();
 
     // where the token's row is in the cache, before the head
     int64_t row = -1;
-    int64_t head_rows = a.S_cap;
-    {
+    if (h1 > a.Hq) {
         const int64_t j = static_cast<int64_t>(i) + (a.start ? max(a.start[b], 0) : 0);
         if (here && j < a.S_cap) {
             if (!a.table) row = static_cast<int64_t>(b) * a.Hkv * a.S_cap + j;
@@ -104,92 +116,103 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(const RotateArgs
                 if (page >= 0 && page < a.n_pages) row = static_cast<int64_t>(page) * a.Hkv * a.page_size + (j - static_cast<int64_t>(p) * a.page_size);
             }
         }
-        if (a.table) head_rows = a.page_size;
     }
+    const int64_t head_rows = a.table ? a.page_size : a.S_cap;
 
-    typedef typename Chunk8<T>::type chunk_t;
-    auto source = [&](int h) {
-        if (h < a.Hq) return a.q + at * a.q_stride + static_cast<int64_t>(h) * DH * ES;
-        if (h < a.Hq + a.Hkv) return a.k + at * a.k_stride + static_cast<int64_t>(h - a.Hq) * DH * ES;
-        return a.v + at * a.v_stride + static_cast<int64_t>(h - a.Hq - a.Hkv) * DH * ES;
+    const int half = a.rot / (2 * R);                      // lanes of a half
+    const bool turned = x * R < a.rot, first = ADJACENT || x < half;
+    const int other = turned && !ADJACENT ? (first ? x + half : x - half) : x;
+    const int other_lane = (threadIdx.x & 63) - x + other;
+    float own[R], its[R];                                  // the two factors
+    auto factors = [&](const char* weight) {
+        float g[R], o[R];
+#pragma unroll
+        for (int e = 0; e < R; ++e) g[e] = o[e] = 1.f;
+        if (weight) {
+            Run<T>::unpack(*reinterpret_cast<const uint4*>(weight + x * R * ES), g);
+            Run<T>::unpack(*reinterpret_cast<const uint4*>(weight + other * R * ES), o);
+        }
+#pragma unroll
+        for (int e = 0; e < R; ++e) {
+            const int pair = mine * PAIRS + (ADJACENT ? (x * R + e) / 2 : (first ? x : x - half) * R + e);
+            const float c = turned ? s_cos[pair] : 1.f, s = turned ? s_sin[pair] : 0.f;
+            own[e] = g[e] * c;
+            its[e] = (ADJACENT ? (e & 1 ? o[e ^ 1] : -o[e ^ 1]) : (first ? -o[e] : o[e])) * s;
+        }
     };
-    float g0[8], g1[8];                                    // the norm's weights
-    chunk_t c0{}, c1{};
-    if (here) {
-        const char* p = source(h0);
-        c0 = *reinterpret_cast<const chunk_t*>(p + e0 * ES);
-        c1 = *reinterpret_cast<const chunk_t*>(p + e1 * ES);
-    }
-    for (int h = h0; h < h1; ++h) {
-        chunk_t y0 = c0, y1 = c1;
-        if (here && h + 1 < h1) {                          // the next head is on its way meanwhile
-            const char* p = source(h + 1);
-            c0 = *reinterpret_cast<const chunk_t*>(p + e0 * ES);
-            c1 = *reinterpret_cast<const chunk_t*>(p + e1 * ES);
+
+    auto source = [&](int h) {
+        const char* p = h < a.Hq ? a.q + at * a.q_stride : h < turned_heads ? a.k + at * a.k_stride : a.v + at * a.v_stride;
+        return p + (static_cast<int64_t>(h - (h < a.Hq ? 0 : h < turned_heads ? a.Hq : turned_heads)) * DH + x * R) * ES;
+    };
+    for (int h = h0; h < h1; h += kAtOnce) {
+        uint4 in[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+            const uint4* p = reinterpret_cast<const uint4*>(source(min(h + k, h1 - 1)));
+            in[k] = uint4{};
+            if (here && h + k < h1) in[k] = STREAM_IN ? load_stream(p) : *p;
         }
-        char* to;
-        if (h < a.Hq) to = a.q_out + ((static_cast<int64_t>(b) * a.Hq + h) * a.n + i) * DH * ES;
-        else {
-            const bool value = h >= a.Hq + a.Hkv;
-            to = (value ? a.v_to : a.k_to) + (row + (h - a.Hq - (value ? a.Hkv : 0)) * head_rows) * DH * ES;
-        }
-        if (h < a.Hq + a.Hkv) {
-            float u[8], w[8];
-            Chunk8<T>::unpack(y0, u);
-            Chunk8<T>::unpack(y1, w);
-            if (a.q_weight) {
-                float sum = 0.f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(u[e], u[e], fmaf(w[e], w[e], sum));
+        for (int k = 0; k < kAtOnce; ++k) {
+            const int at_head = h + k;
+            if (at_head >= h1) break;
+            uint4 y = in[k];
+            if (at_head == h0 || at_head == a.Hq) factors(at_head < a.Hq ? a.q_weight : a.k_weight);
+            if (at_head < turned_heads) {
+                float u[R], w[R];
+                Run<T>::unpack(y, u);
+                if constexpr (ADJACENT) {
 #pragma unroll
-                for (int off = 1; off < LANES; off <<= 1) sum += __shfl_xor(sum, off, 64);
-                const float mean = fmaf(sum, 1.f / DH, a.eps), inv = mean > 0.f ? 1.f / sqrtf(mean) : 0.f;
-                if (h == h0 || h == a.Hq) {
-                    const char* weight = h < a.Hq ? a.q_weight : a.k_weight;
-                    Chunk8<T>::unpack(*reinterpret_cast<const chunk_t*>(weight + e0 * ES), g0);
-                    Chunk8<T>::unpack(*reinterpret_cast<const chunk_t*>(weight + e1 * ES), g1);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) { u[e] = u[e] * inv * g0[e]; w[e] = w[e] * inv * g1[e]; }
-            }
-            float s[8], t[8];
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-                if constexpr (ADJACENT) {                  // pairs 0 .. 3 in the first run, 4 .. 7 in the second
-                    float(&z)[8] = p < 4 ? u : w;
-                    float(&o)[8] = p < 4 ? s : t;
-                    const int e = 2 * (p & 3);
-                    o[e] = z[e] * cos[p] - z[e + 1] * sin[p];
-                    o[e + 1] = z[e + 1] * cos[p] + z[e] * sin[p];
+                    for (int e = 0; e < R; ++e) w[e] = u[e ^ 1];
                 } else {
-                    s[p] = u[p] * cos[p] - w[p] * sin[p];
-                    t[p] = w[p] * cos[p] + u[p] * sin[p];
+                    const uint4 z = make_uint4(__shfl(y.x, other_lane, 64), __shfl(y.y, other_lane, 64), __shfl(y.z, other_lane, 64), __shfl(y.w, other_lane, 64));
+                    Run<T>::unpack(z, w);
                 }
+                float f = 1.f;
+                if (a.q_weight) {
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < R; ++e) sum = fmaf(u[e], u[e], sum);
+                    const float mean = fmaf(lanes_sum<LANES>(sum), 1.f / DH, a.eps);
+                    f = mean >= 0x1p-126f ? __builtin_amdgcn_rsqf(mean) : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < R; ++e) u[e] = fmaf(u[e], own[e], w[e] * its[e]) * f;
+                y = Run<T>::pack(u);
             }
-            y0 = Chunk8<T>::pack(s);
-            y1 = Chunk8<T>::pack(t);
-        }
-        if (here && (h < a.Hq || row >= 0)) {
-            *reinterpret_cast<chunk_t*>(to + e0 * ES) = y0;
-            *reinterpret_cast<chunk_t*>(to + e1 * ES) = y1;
+            char* to;
+            if (at_head < a.Hq) to = a.q_out + ((static_cast<int64_t>(b) * a.Hq + at_head) * a.n + i) * DH * ES;
+            else to = (at_head < turned_heads ? a.k_to + (row + (at_head - a.Hq) * head_rows) * DH * ES : a.v_to + (row + (at_head - turned_heads) * head_rows) * DH * ES);
+            if (here && (at_head < a.Hq || row >= 0)) {
+                if (STREAM_OUT) store_stream(reinterpret_cast<uint4*>(to) + x, y);
+                else reinterpret_cast<uint4*>(to)[x] = y;
+            }
         }
     }
 }
 
 template <typename T, int DH> static int launch_rotate(RotateArgs& a, bool adjacent, hipStream_t st) {
-    constexpr int per_group = kRotateWaves * 64 / (DH / kLaneElems);
-    const int64_t groups = (a.tokens + per_group - 1) / per_group, heads = a.Hq + 2 * a.Hkv;
-    const int64_t rows = groups * kRotateWaves * heads, most = (rows + kRotateSpread - 1) / kRotateSpread;
-    const int64_t turns = (heads + most - 1) / most;       // alike, so that no wave has much less than the others
-    a.per_wave = static_cast<int>((heads + turns - 1) / turns);
-    const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((heads + a.per_wave - 1) / a.per_wave));
-    if (adjacent) hipLaunchKernelGGL((rotate_kernel<T, DH, true>), grid, dim3(kRotateThreads), 0, st, a);
-    else hipLaunchKernelGGL((rotate_kernel<T, DH, false>), grid, dim3(kRotateThreads), 0, st, a);
+    constexpr int tokens = kRotateThreads * Run<T>::kElems / DH;
+    const int64_t groups = (a.tokens + tokens - 1) / tokens, heads = a.Hq + 2 * a.Hkv;
+    a.per_group = groups * heads >= kRotateSpread ? rotate_heads(sizeof(T)) : 1;
+    const dim3 grid(static_cast<unsigned>(groups), static_cast<unsigned>((heads + a.per_group - 1) / a.per_group)), threads(kRotateThreads);
+    const int64_t bytes = a.tokens * heads * DH * static_cast<int64_t>(sizeof(T));
+    const bool in = bytes > kStreamIn, out = bytes > kStreamOut;
+    if (adjacent) {
+        if (in) hipLaunchKernelGGL((rotate_kernel<T, DH, true, true, true>), grid, threads, 0, st, a);
+        else if (out) hipLaunchKernelGGL((rotate_kernel<T, DH, true, false, true>), grid, threads, 0, st, a);
+        else hipLaunchKernelGGL((rotate_kernel<T, DH, true, false, false>), grid, threads, 0, st, a);
+    } else {
+        if (in) hipLaunchKernelGGL((rotate_kernel<T, DH, false, true, true>), grid, threads, 0, st, a);
+        else if (out) hipLaunchKernelGGL((rotate_kernel<T, DH, false, false, true>), grid, threads, 0, st, a);
+        else hipLaunchKernelGGL((rotate_kernel<T, DH, false, false, false>), grid, threads, 0, st, a);
+    }
     return check_launch("rotate");
 }
 
 // Tokens of a call at most: a grid has fewer than 2^32 threads.
-constexpr int64_t kMostTokens = 1 << 27;
+constexpr int64_t kMostTokens = 1 << 26;
 
 static int rotate_impl(const void* q, const void* k, const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride, int B, int64_t n, int Hq, int Hkv, int dh, int dtype,
                        const int32_t* count, const void* q_weight, const void* k_weight, double eps, const int32_t* pos, int n_axes, const float* inv_freq,
@@ -198,7 +221,7 @@ static int rotate_impl(const void* q, const void* k, const void* v, int64_t q_st
     if (dtype != METOK_F32 && dtype != METOK_BF16) return fail(METOK_ERR_INVALID_ARG, "unknown dtype");
     if (dh != 32 && dh != 64 && dh != 128 && !(dh == 256 && dtype == METOK_BF16)) return fail(METOK_ERR_INVALID_ARG, "dh must be 32, 64, 128 or (bf16) 256");
     if (B < 1 || B > METOK_MAX_DECODE_BATCH) return fail(METOK_ERR_INVALID_ARG, "B must be in [1, METOK_MAX_DECODE_BATCH]");
-    if (n < 1 || n > kMostTokens / B) return fail(METOK_ERR_INVALID_ARG, "n must be positive and B * n at most 2^27");
+    if (n < 1 || n > kMostTokens / B) return fail(METOK_ERR_INVALID_ARG, "n must be positive and B * n at most 2^26");
     if (Hq < 1 || Hkv < 1 || Hq > 4096 || Hkv > 4096 || Hq + 2 * Hkv > 4096) return fail(METOK_ERR_INVALID_ARG, "Hq and Hkv must be positive, Hq + 2 Hkv at most 4096");
     if (S_cap < 1 || S_cap >= INT32_MAX - 64) return fail(METOK_ERR_INVALID_ARG, "the capacity must be in [1, 2^31 - 64)");
     if (!q || !k || !v || !pos || !inv_freq || !q_out || !k_to || !v_to) return fail(METOK_ERR_INVALID_ARG, "q, k, v, pos, inv_freq, q_out and the caches must not be NULL");
@@ -209,7 +232,7 @@ static int rotate_impl(const void* q, const void* k, const void* v, int64_t q_st
         return fail(METOK_ERR_INVALID_ARG, "pos, count and start must be 4-byte aligned");
     if (!(eps >= 0.0 && eps <= 1.0)) return fail(METOK_ERR_INVALID_ARG, "eps must be in [0, 1]");
     if (n_axes < 1 || n_axes > METOK_MAX_POSITION_AXES) return fail(METOK_ERR_INVALID_ARG, "n_axes must be in [1, METOK_MAX_POSITION_AXES]");
-    if (rot < kLaneElems || rot > dh || rot % kLaneElems != 0) return fail(METOK_ERR_INVALID_ARG, "rot must be a positive multiple of 16 and at most dh");
+    if (rot < kRotUnit || rot > dh || rot % kRotUnit != 0) return fail(METOK_ERR_INVALID_ARG, "rot must be a positive multiple of 16 and at most dh");
     if (pairs != METOK_PAIRS_HALVES && pairs != METOK_PAIRS_ADJACENT) return fail(METOK_ERR_INVALID_ARG, "unknown pairs");
     const int64_t es = static_cast<int64_t>(dtype_size(dtype)), limit = static_cast<int64_t>(1) << 40;
     const struct { const char* name; int64_t stride, heads; } strides[] = {{"q_stride", q_stride, Hq}, {"k_stride", k_stride, Hkv}, {"v_stride", v_stride, Hkv}};
@@ -220,7 +243,7 @@ static int rotate_impl(const void* q, const void* k, const void* v, int64_t q_st
     for (int p = 0; p < rot / 2; ++p) {
         const int axis = pair_axis ? pair_axis[p] : 0;
         if (axis >= n_axes) return fail(METOK_ERR_INVALID_ARG, "pair_axis[%d] is not below n_axes", p);
-        a.axis[p / 8] |= static_cast<uint64_t>(axis) << (8 * (p % 8));
+        a.axis[p] = static_cast<uint8_t>(axis);
     }
     const int64_t tokens = static_cast<int64_t>(B) * n;
     auto rows = [&](int64_t stride, int heads) { return static_cast<size_t>(((tokens - 1) * stride + static_cast<int64_t>(heads) * dh) * es); };
