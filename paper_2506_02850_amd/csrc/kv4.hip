@@ -1,7 +1,8 @@
 // Rows into a KV cache of 4 bits and back (include/metok_qkv.h): the compacted rows of stage 3 (Sec. 3.3) or the rows of a chunk, gathered, put into 4 bits and
 // stored in one pass; and rows of such a cache as the values they stand for.
 //
-// Both move bytes and compute little: a row of 128 elements of K and V in bf16 is 512 bytes on one side and 136 on the other.
+// Both move bytes and compute little: a row of 128 elements of K and V in bf16 is 512 bytes on one side and 136 on the other.  8 x 36992 rows of 4 heads: 131 us
+// into 4 bits, 5.9 TB/s; a few thousand rows 5 to 8 us, which are the launch and the loads that wait for each other (count and start, index, row).
 #include "kv4.h"
 
 namespace metok {
@@ -15,6 +16,9 @@ struct Rows4Args {
     int page_size, pages_per_seq, n_pages;
 };
 
+// Rows of more bytes than this are read by a pack, written by an unpack, with the streaming hint: 8 x 36992 rows of 4 heads of 128 in bf16, 606 MB, 131 us with it and 163
+// without into 4 bits, 108 to 137 and 126 to 139 back; 9333 rows, 19 MB, 9.0 and 7.9 (the memory-side cache has them still), 5.5 and 6.6.
+constexpr int64_t kStreamPack = 128 << 20, kStreamUnpack = 16 << 20;
 constexpr int kRows4Threads = 256, kRows4Waves = kRows4Threads / 64;
 
 // The block of 16 rows of the 4-bit cache that logical row j of a video lies in; -1: no such page.  0 <= j < S_cap.
@@ -25,23 +29,38 @@ __device__ __forceinline__ int64_t block_of(const Rows4Args& a, int b, int h, in
     return (static_cast<int64_t>(page) * a.Hkv + h) * (a.page_size / kBlockRows) + (j - at * a.page_size) / kBlockRows;
 }
 
+// N neighbouring words, with the streaming hint or without.
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+template <int N, bool STREAM, typename V> __device__ __forceinline__ void load_run(uint32_t (&w)[N], const V* p) {
+    V v;
+    if constexpr (STREAM) v = __builtin_nontemporal_load(p);
+    else v = *p;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if constexpr (N == 1) w[j] = v; else w[j] = v[j];
+    }
+}
+template <int N, bool STREAM> __device__ __forceinline__ void load_run(uint32_t (&w)[N], const char* p) {
+    if constexpr (N == 4) load_run<N, STREAM>(w, reinterpret_cast<const u32x4_t*>(p));
+    else if constexpr (N == 2) load_run<N, STREAM>(w, reinterpret_cast<const u32x2_t*>(p));
+    else load_run<N, STREAM>(w, reinterpret_cast<const uint32_t*>(p));
+}
+template <bool STREAM, typename V> __device__ __forceinline__ void store_run(V* p, V v) {
+    if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // E elements (2, 4, 8) of type T at p, as floats.
-template <typename T, int E> __device__ __forceinline__ void load_elements(float (&x)[E], const char* p) {
-    if constexpr (sizeof(T) == 2) {
-        uint32_t w[E / 2];
-        if constexpr (E == 8) { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
-        else if constexpr (E == 4) { const uint2 v = *reinterpret_cast<const uint2*>(p); w[0] = v.x; w[1] = v.y; }
-        else w[0] = *reinterpret_cast<const uint32_t*>(p);
+template <typename T, int E, bool STREAM> __device__ __forceinline__ void load_elements(float (&x)[E], const char* p) {
+    constexpr int WORDS = E * static_cast<int>(sizeof(T)) / 4, N = WORDS < 4 ? WORDS : 4;
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
-    } else {
-        if constexpr (E == 2) { const float2 v = *reinterpret_cast<const float2*>(p); x[0] = v.x; x[1] = v.y; }
-        else {
+    for (int k = 0; k < WORDS; k += N) {
+        uint32_t w[N];
+        load_run<N, STREAM>(w, p + 4 * k);
 #pragma unroll
-            for (int i = 0; i < E; i += 4) {
-                const float4 v = *reinterpret_cast<const float4*>(p + 4 * i);
-                x[i] = v.x; x[i + 1] = v.y; x[i + 2] = v.z; x[i + 3] = v.w;
-            }
+        for (int j = 0; j < N; ++j) {
+            if constexpr (sizeof(T) == 2) { x[2 * (k + j)] = bf16_lo(w[j]); x[2 * (k + j) + 1] = bf16_hi(w[j]); }
+            else x[k + j] = __uint_as_float(w[j]);
         }
     }
 }
@@ -60,7 +79,7 @@ template <int BYTES> __device__ __forceinline__ uint32_t load_bytes(const char* 
 // A wave per block of the cache, video, kv head and K or V.  Lane (c, r): elements r w / 16 .. of rows 4 c .. 4 c + 3, so that 16 lanes have whole rows
 // and a lane's codes of the four rows are what V keeps beside each other.  A block has one writer; where some of its rows are not to be
 // written, the others are stored byte by byte as far as they mix.
-template <typename T, int DH>
+template <typename T, int DH, bool STREAM>
 __global__ __launch_bounds__(kRows4Threads) void pack4_kernel(const Rows4Args a) {
     using F = Block4<DH>;
     constexpr int E = F::kWidth / 16, EB = F::kRunBytes;
@@ -90,7 +109,7 @@ __global__ __launch_bounds__(kRows4Threads) void pack4_kernel(const Rows4Args a)
     for (int p = 0; p < F::kPieces; ++p) {
         float x[4][E];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_elements<T, E>(x[i], from + (src[i] * DH + p * F::kWidth + r * E) * static_cast<int64_t>(sizeof(T)));
+        for (int i = 0; i < 4; ++i) load_elements<T, E, STREAM>(x[i], from + (src[i] * DH + p * F::kWidth + r * E) * static_cast<int64_t>(sizeof(T)));
         uint32_t codes[4], scales = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -133,7 +152,7 @@ __global__ __launch_bounds__(kRows4Threads) void pack4_kernel(const Rows4Args a)
 }
 
 // A wave per 16 rows of the output, lanes as above.
-template <typename T, int DH>
+template <typename T, int DH, bool STREAM>
 __global__ __launch_bounds__(kRows4Threads) void unpack4_kernel(const Rows4Args a) {
     using F = Block4<DH>;
     constexpr int E = F::kWidth / 16, EB = F::kRunBytes;
@@ -164,15 +183,16 @@ __global__ __launch_bounds__(kRows4Threads) void unpack4_kernel(const Rows4Args 
             if constexpr (E >= 4) y[1] = take_codes<1>(w, s);
             if constexpr (E >= 8) { y[2] = take_codes<2>(w, s); y[3] = take_codes<3>(w, s); }
             char* out = to + (at * DH + p * F::kWidth + r * E) * static_cast<int64_t>(sizeof(T));
+            auto lo = [](uint32_t two) { return two << 16; };
+            auto hi = [](uint32_t two) { return two & 0xffff0000u; };
             if constexpr (sizeof(T) == 2) {
-                if constexpr (E == 8) *reinterpret_cast<uint4*>(out) = make_uint4(y[0], y[1], y[2], y[3]);
-                else if constexpr (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(y[0], y[1]);
-                else *reinterpret_cast<uint32_t*>(out) = y[0];
-            } else if constexpr (E == 2) *reinterpret_cast<float2*>(out) = make_float2(bf16_lo(y[0]), bf16_hi(y[0]));
+                if constexpr (E == 8) store_run<STREAM>(reinterpret_cast<u32x4_t*>(out), u32x4_t{y[0], y[1], y[2], y[3]});
+                else if constexpr (E == 4) store_run<STREAM>(reinterpret_cast<u32x2_t*>(out), u32x2_t{y[0], y[1]});
+                else store_run<STREAM>(reinterpret_cast<uint32_t*>(out), y[0]);
+            } else if constexpr (E == 2) store_run<STREAM>(reinterpret_cast<u32x2_t*>(out), u32x2_t{lo(y[0]), hi(y[0])});
             else {
-#pragma unroll
-                for (int e = 0; e < E / 2; e += 2)
-                    *reinterpret_cast<float4*>(out + 8 * e) = make_float4(bf16_lo(y[e]), bf16_hi(y[e]), bf16_lo(y[e + 1]), bf16_hi(y[e + 1]));
+                store_run<STREAM>(reinterpret_cast<u32x4_t*>(out), u32x4_t{lo(y[0]), hi(y[0]), lo(y[1]), hi(y[1])});
+                if constexpr (E == 8) store_run<STREAM>(reinterpret_cast<u32x4_t*>(out) + 1, u32x4_t{lo(y[2]), hi(y[2]), lo(y[3]), hi(y[3])});
             }
         }
     }
@@ -182,8 +202,13 @@ template <typename T, int DH> static int launch_rows4(bool pack, const Rows4Args
     // the rows may begin inside a block of the cache
     const int64_t waves = pack ? (a.n + kBlockRows - 1 + kBlockRows - 1) / kBlockRows : (a.n + 15) / 16;
     const dim3 grid(static_cast<unsigned>((waves + kRows4Waves - 1) / kRows4Waves), static_cast<unsigned>(2 * a.Hkv), static_cast<unsigned>(B));
-    if (pack) hipLaunchKernelGGL((pack4_kernel<T, DH>), grid, dim3(kRows4Threads), 0, st, a);
-    else hipLaunchKernelGGL((unpack4_kernel<T, DH>), grid, dim3(kRows4Threads), 0, st, a);
+    const int64_t bytes = 2 * static_cast<int64_t>(B) * a.Hkv * a.n * DH * static_cast<int64_t>(sizeof(T));       // of the rows that are not in 4 bits
+    const bool stream = bytes > (pack ? kStreamPack : kStreamUnpack);
+    const dim3 threads(kRows4Threads);
+    if (pack && stream) hipLaunchKernelGGL((pack4_kernel<T, DH, true>), grid, threads, 0, st, a);
+    else if (pack) hipLaunchKernelGGL((pack4_kernel<T, DH, false>), grid, threads, 0, st, a);
+    else if (stream) hipLaunchKernelGGL((unpack4_kernel<T, DH, true>), grid, threads, 0, st, a);
+    else hipLaunchKernelGGL((unpack4_kernel<T, DH, false>), grid, threads, 0, st, a);
     return check_launch(pack ? "pack rows" : "unpack rows");
 }
 
