@@ -26,15 +26,29 @@ __device__ __forceinline__ void add_sum(float& m, float& l, float m2, float l2, 
     m = to;
 }
 
-// The workers of a query head's pair, and the place of their partial results.
+// The workers of a query head's pair, and the place of their partial results.  Of the workgroups between the first worker's and the last one's, teams leave one part each.
 struct HeadParts {
-    int first, n, rows, row;
-    __device__ __forceinline__ int64_t slot(int p) const { return static_cast<int64_t>(2 * (first + p) + (p == 0)) * rows + row; }
+    int first, n, rows, row, alone, teams;                 // parts of the first worker's workgroup (of all, without teams), and of the teams behind it
+    __device__ __forceinline__ int64_t slot(int p) const {
+        int worker = first + p;
+        if (p >= alone) {
+            const int group = first / kAttendWaves + 1 + min(p - alone, teams);
+            worker = group * kAttendWaves + max(p - alone - teams, 0);
+        }
+        return static_cast<int64_t>(2 * worker + (p == 0)) * rows + row;
+    }
 };
 __device__ __forceinline__ HeadParts parts_of(const DecodeArgs& a, int b, int head) {
     const int kvh = head / a.group, qi = head - kvh * a.group, rb = qi / a.block_rows;
     const int2 w = a.pair_workers[(static_cast<int64_t>(b) * a.Hkv + kvh) * a.row_blocks + rb];
-    return {w.x, w.y - w.x + 1, a.rows, qi - rb * a.block_rows};
+    const int between = w.y / kAttendWaves - w.x / kAttendWaves - 1;       // workgroups
+    HeadParts p{w.x, w.y - w.x + 1, a.rows, qi - rb * a.block_rows, w.y - w.x + 1, 0};
+    if (a.teams && between > 0) {
+        p.alone = kAttendWaves - w.x % kAttendWaves;
+        p.teams = between;
+        p.n -= (kAttendWaves - 1) * between;
+    }
+    return p;
 }
 
 template <typename T, int DH>
@@ -253,6 +267,7 @@ int attend_call(const AttendCall& c, const AttendPlan& plan, int (*launch)(const
     a.pair_workers = plan.joined || weight ? reinterpret_cast<int2*>(ws + plan.pair_workers) : nullptr;
     a.part_ml = reinterpret_cast<float*>(ws + plan.part_ml); a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
     a.norm = reinterpret_cast<float2*>(ws + plan.lse2); a.logits = reinterpret_cast<float*>(ws + plan.logits);
+    a.teams = plan.teams;
     a.weight_stride = weight_stride; a.logit_stride = plan.logit_stride;
     a.B = B; a.Hq = Hq; a.Hkv = Hkv; a.group = Hq / Hkv; a.row_blocks = plan.row_blocks; a.rows = plan.rows; a.block_rows = plan.block_rows;
     a.S_cap = static_cast<int>(S_cap); a.page_size = page_size; a.pages_per_seq = pages_per_seq; a.n_pages = static_cast<int>(n_pages);

@@ -37,6 +37,7 @@ struct DecodeArgs {
     float scale;                 // without cap: of the logits in the log2 domain; with cap: scale / cap
     float cap;                   // cap in the log2 domain, 0: none
     int join_blocks, join_lanes, weight_blocks, head_lanes;      // of decode_join_kernel
+    int teams;                   // the workers of a workgroup follow each other, and one that is in the middle of a pair leaves one part, its first worker's
 };
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -53,8 +54,8 @@ __device__ __forceinline__ int rows_before(const DecodeArgs& a, int b) {
     return n < 0 ? 0 : (n > a.S_cap ? a.S_cap : n);
 }
 
-// Where a worker begins: video, its tiles and rows, unit of all its pairs; and how many units it has.
-struct Place { int b, n, tiles, at, left; };
+// Where a worker begins: video, its tiles and rows, unit of all its pairs; how many units it has; and all units of the call.
+struct Place { int b, n, tiles, at, left; int64_t all; };
 
 // Goes through the videos, 64 a step, one to a lane.  An empty video has a tile, too, without rows.  Uniform over the wave.  left = 0: there is
 // no such worker.
@@ -74,7 +75,7 @@ __device__ __forceinline__ Place find_place(const DecodeArgs& a, int worker) {
     };
     for (int b0 = 0; b0 < a.B; b0 += 64) total += look(b0);
     const int64_t all = static_cast<int64_t>(total) * heads, first = DEAL::first(worker, all);
-    Place p{0, 0, 0, 0, static_cast<int>(DEAL::first(worker + 1, all) - first)};
+    Place p{0, 0, 0, 0, static_cast<int>(DEAL::first(worker + 1, all) - first), all};
     if (worker >= DEAL::workers(all)) p.left = 0;
     if (p.left <= 0) return p;
     int base = 0;

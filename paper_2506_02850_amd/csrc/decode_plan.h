@@ -55,14 +55,15 @@ struct AttendPlan {
     int64_t workers;       // at most
     bool whole;            // a workgroup to a pair, no second launch and no workspace
     bool joined;           // false: every pair is one tile, whatever the lengths
+    bool teams;            // a workgroup in the middle of a pair leaves one part
     int64_t logit_stride;  // logits of a (video, query head), 0: not kept
     size_t pair_workers, part_ml, part_o, lse2, logits, bytes;       // offsets in the workspace, and its size
                            // (lse2: a head's maximum and 1 / sum, what the logarithm of its sum is made of)
 };
 
 // What the split goes by beside the shapes: cache rows of a tile, workgroups of a large call, blocks of 16 query heads that a wave takes at a time where a
-// kv head has more than one, and up to how many tiles a pair is left to one workgroup.
-struct AttendSplit { int tile, groups, blocks, whole; };
+// kv head has more than one, up to how many tiles a pair is left to one workgroup, and whether the workers of a workgroup may join what they leave of a pair.
+struct AttendSplit { int tile, groups, blocks, whole; bool teams; };
 
 // `capacity` rows at most, one more with a new row.
 constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh, const AttendSplit& split, bool with_weight) {
@@ -80,6 +81,7 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
     const int groups = split.groups;
     const int64_t few = ((most + kAttendPairCost) * p.pairs + kAttendMinTiles - 1) / kAttendMinTiles;      // workers, with a workgroup each
     p.grid = few < groups ? few : groups;
+    p.teams = split.teams && few > groups;
     p.workers = static_cast<int64_t>(groups) * kAttendWaves;
     const int rounded = p.tile > 32 ? p.tile : 32;                                   // whole tiles are written
     p.logit_stride = with_weight ? (capacity + 1 + rounded - 1) / rounded * rounded : 0;
@@ -101,14 +103,14 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
     return p;
 }
 constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int dh, int esize, bool with_weight) {
-    return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole}, with_weight);
+    return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole, false}, with_weight);
 }
 
 // The same over a cache in 4 bits (kv4_attention.hip): a row has a quarter of the bytes, so there are two waves to a SIMD.
 constexpr int kAttend4Tile = 32, kAttend4Groups = 512;
 constexpr int kAttend4Whole = 32;
 constexpr AttendPlan plan_attend4(int B, int Hq, int Hkv, int64_t capacity, int dh, bool with_weight) {
-    return plan_split(B, Hq, Hkv, capacity, dh, {kAttend4Tile, kAttend4Groups, 1, kAttend4Whole}, with_weight);
+    return plan_split(B, Hq, Hkv, capacity, dh, {kAttend4Tile, kAttend4Groups, 1, kAttend4Whole, true}, with_weight);
 }
 
 }  // namespace metok

@@ -42,7 +42,10 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     constexpr int QP = BF16 ? 1 : 3, PP = BF16 ? 2 : 3;    // parts of a query, of a probability
     static_assert(NT % 2 == 0 && KW == EB, "32 rows to a product; a lane has as much of K as of V");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
-    const int worker = wave * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+    // neighbouring workers on different CUs where there are few, so that few tiles are spread over all of them; in one workgroup where there are many, so that
+    // they can join what they leave of a pair that none of them begins or ends
+    const int worker = a.teams ? static_cast<int>(blockIdx.x) * kAttendWaves + wave : wave * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
+    bool team = false;                                     // the workgroup is in the middle of a pair
     const bool fresh = a.k_new != nullptr;
     const scalar_ints lens = reinterpret_cast<scalar_ints>(reinterpret_cast<uintptr_t>(a.len));
     // of the new row: K's and V's codes in the order of the elements, then the scales
@@ -62,7 +65,8 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         at.t = wave * at.tiles / kAttendWholeWaves;
         left = (wave + 1) * at.tiles / kAttendWholeWaves - at.t;
     } else {
-        const Place place = find_place<TILE, Deal<kAttend4Groups>>(a, worker);
+        typedef Deal<kAttend4Groups> D;
+        const Place place = find_place<TILE, D>(a, worker);
         if (place.left <= 0) return;
         at.b = __builtin_amdgcn_readfirstlane(place.b);
         at.tiles = __builtin_amdgcn_readfirstlane(place.tiles);
@@ -73,6 +77,11 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         at.rb = hr - at.kvh * a.row_blocks;
         at.t = __builtin_amdgcn_readfirstlane(place.at) - hr * units;
         left = __builtin_amdgcn_readfirstlane(place.left);
+        if (a.teams) {
+            const int64_t mine = D::first(worker, place.all), group = static_cast<int64_t>(blockIdx.x) * kAttendWaves;
+            const int64_t begins = at.t - (mine - D::first(group, place.all)), ends = at.t + (D::first(group + kAttendWaves, place.all) - mine);
+            team = __builtin_amdgcn_readfirstlane(begins > 0 && ends < at.tiles);
+        }
     }
     int n_ahead = WHOLE ? 0 : lens[min(at.b + 1, a.B - 1)];
     auto advance = [&](Cursor x) {
@@ -135,7 +144,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         return f;
     };
     uint32_t kf[NT][P][KW], vf[NT][P][KW], ks[NT][P], vs[NT][P];
-    const uint32_t k_code = r * F::kRowBytes + c * (4 * KW), k_scale = F::kScales + (r >> 2) * 4 * F::kGroups + c * F::kWidth / 128 * 4 + (r & 3);
+    const uint32_t k_code = r * F::kRowBytes + c * (4 * KW), k_scale = F::kScales + (r >> 2) * 4 * F::kGroups + c * F::kWidth / 128 * 4, k_byte = 8 * (r & 3);
     const uint32_t v_code = c * 2 * F::kWidth + r * 4 * EB, v_scale = F::kScales + c * 4 * F::kGroups + r * F::kWidth / 512 * 4;
     auto base_of = [&](const Cursor& x, const char* cache, int block) {
         return cache + ((PAGED ? 0 : slab_of(x) * (a.S_cap / kBlockRows)) + block) * F::kBytes;
@@ -148,7 +157,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
 #pragma unroll
             for (int p = 0; p < P; ++p) {
                 load_words<KW, STREAM>(kf[b][p], block + p * F::kPieceBytes + code);
-                ks[b][p] = *reinterpret_cast<const uint8_t*>(block + p * 16 * F::kGroups + scale);
+                ks[b][p] = *reinterpret_cast<const uint32_t*>(block + p * 16 * F::kGroups + scale);        // of four rows, the lane's own in byte r % 4
             }
         }
     };
@@ -226,7 +235,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
                 const bool mine = in == 16 * b + r;
 #pragma unroll
                 for (int i = 0; i < KW; ++i) kf[b][p][i] = mine ? w[i] : kf[b][p][i];
-                ks[b][p] = mine ? scale : ks[b][p];
+                ks[b][p] = mine ? scale << (8 * (r & 3)) : ks[b][p];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool own = in == 16 * b + 4 * c + i;
@@ -284,7 +293,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             s[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int p = 0; p < P; ++p) {
-                const float scale = scale_from(ks[b][p]);
+                const float scale = scale_from((ks[b][p] >> k_byte) & 0xffu);
 #pragma unroll
                 for (int i = 0; i < KW; ++i) {
                     const uint32_t w = kf[b][p][i];
@@ -464,7 +473,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             const Rows rows_next = rows_of(next, pages);
             load_k(next, rows_next);
             take(at, rows, s);
-            if (ends || (!WHOLE && last)) finish(at, begun);
+            if (ends || (!WHOLE && last && !team)) finish(at, begun);
             append(at);
             if (ends && !last) {
                 begun = 0;
@@ -477,8 +486,8 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
             rows = rows_next;
         }
     }
-    if constexpr (WHOLE) {
-        constexpr int W = kAttendWholeWaves, PITCH = DH + 4, LPR = DH / 4;       // 4 more: rows 16 bytes apart in the banks
+    if (WHOLE || team) {                                   // the waves' sums become one
+        constexpr int W = WHOLE ? kAttendWholeWaves : kAttendWaves, PITCH = DH + 4, LPR = DH / 4;       // 4 more: rows 16 bytes apart in the banks
         __shared__ float4 s_o[W * kAttendRows * PITCH / 4];
         __shared__ float2 s_ml[W][kAttendRows];
         const float sum = swap32_add(swap16_add(l, l), swap16_add(l, l));
@@ -506,12 +515,18 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
                 total = fmaf(part.y, f, total);
                 o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
             }
-            const float inv = total == 0.f ? 0.f : 1.f / total;
-            const int64_t head = static_cast<int64_t>(at.b) * a.Hq + first_head(at) + row;
-            char* out = a.out + head * RB + 4 * x * static_cast<int>(sizeof(T));
-            if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-            else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-            if (x == 0 && a.lse) a.lse[head] = total == 0.f ? -INFINITY : fmaf(ref, scale, log2_of(total)) * 0.693147180559945309f;
+            if constexpr (WHOLE) {
+                const float inv = total == 0.f ? 0.f : 1.f / total;
+                const int64_t head = static_cast<int64_t>(at.b) * a.Hq + first_head(at) + row;
+                char* out = a.out + head * RB + 4 * x * static_cast<int>(sizeof(T));
+                if constexpr (BF16) *reinterpret_cast<uint2*>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+                else *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+                if (x == 0 && a.lse) a.lse[head] = total == 0.f ? -INFINITY : fmaf(ref, scale, log2_of(total)) * 0.693147180559945309f;
+            } else {
+                const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) * kAttendWaves * a.rows + row;
+                *reinterpret_cast<float4*>(a.part_o + slot * DH + 4 * x) = o;
+                if (x == 0) reinterpret_cast<float2*>(a.part_ml)[slot] = make_float2(top, total);
+            }
         }
     }
 }
