@@ -106,8 +106,12 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
     return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole, false}, with_weight);
 }
 
-// The same over a cache in 4 bits (kv4_attention.hip): a row has a quarter of the bytes, so there are two waves to a SIMD.
+// The same over a cache in 4 bits (kv4_attention.hip).  A row has a quarter of the bytes, so it takes two waves to a SIMD to keep enough of them on their way, and
+// tiles of 32 rows at any width (28 heads on 4 of 128, 8 x 36992 rows: 31.3 us with 512 workgroups, 41.3 with 256; 32 videos of 0 to 8191 rows 15.6 and 19.5.  Tiles
+// of 64 rows in 256 workgroups take as long at 8 x 36992, but 2307 rows 6.2 us against 5.4, 8 x 3000 of 256 elements 11.3 against 8.4).
 constexpr int kAttend4Tile = 32, kAttend4Groups = 512;
+// A pair per workgroup up to 32 tiles, as above.  28 heads on 4 of 128: 120 rows 5.1 us (10.4 split and joined), 1000 rows 8.3 (10.6), 16 of them 9.1
+// (12.0), 64 of them 10.8 (19.6); 2000 rows 12.5 (9.9), 16 of them 14.0 (13.4), 64 of them 16.5 (24.2).
 constexpr int kAttend4Whole = 32;
 constexpr AttendPlan plan_attend4(int B, int Hq, int Hkv, int64_t capacity, int dh, bool with_weight) {
     return plan_split(B, Hq, Hkv, capacity, dh, {kAttend4Tile, kAttend4Groups, 1, kAttend4Whole, true}, with_weight);
