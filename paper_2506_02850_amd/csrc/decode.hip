@@ -26,29 +26,17 @@ __device__ __forceinline__ void add_sum(float& m, float& l, float m2, float l2, 
     m = to;
 }
 
-// The workers of a query head's pair, and the place of their partial results.  Of the workgroups between the first worker's and the last one's, teams leave one part each.
+// The parts of a query head's result, and the place of each among all query rows of all parts.
 struct HeadParts {
-    int first, n, rows, row, alone, teams;                 // parts of the first worker's workgroup (of all, without teams), and of the teams behind it
-    __device__ __forceinline__ int64_t slot(int p) const {
-        int worker = first + p;
-        if (p >= alone) {
-            const int group = first / kAttendWaves + 1 + min(p - alone, teams);
-            worker = group * kAttendWaves + max(p - alone - teams, 0);
-        }
-        return static_cast<int64_t>(2 * worker + (p == 0)) * rows + row;
-    }
+    PairParts pair;
+    int n, rows, row;
+    __device__ __forceinline__ int64_t slot(int p) const { return static_cast<int64_t>(pair.slot(p)) * rows + row; }
 };
 __device__ __forceinline__ HeadParts parts_of(const DecodeArgs& a, int b, int head) {
     const int kvh = head / a.group, qi = head - kvh * a.group, rb = qi / a.block_rows;
     const int2 w = a.pair_workers[(static_cast<int64_t>(b) * a.Hkv + kvh) * a.row_blocks + rb];
-    const int between = w.y / kAttendWaves - w.x / kAttendWaves - 1;       // workgroups
-    HeadParts p{w.x, w.y - w.x + 1, a.rows, qi - rb * a.block_rows, w.y - w.x + 1, 0};
-    if (a.teams && between > 0) {
-        p.alone = kAttendWaves - w.x % kAttendWaves;
-        p.teams = between;
-        p.n -= (kAttendWaves - 1) * between;
-    }
-    return p;
+    const PairParts pair = pair_parts(w.x, w.y, a.teams != 0);
+    return {pair, pair.n, a.rows, qi - rb * a.block_rows};
 }
 
 template <typename T, int DH>

@@ -42,7 +42,31 @@ template <int GROUPS> struct Deal {
         const int64_t at = units < static_cast<int64_t>(kAttendMinTiles) * kWorkers ? worker * kAttendMinTiles : worker * units / kWorkers;
         return at < units ? at : units;
     }
+    // Whether a worker's whole workgroup, of kAttendWaves workers that follow each other, is in the middle of the pair in which the worker begins at tile t.
+    static constexpr bool in_the_middle(int64_t worker, int64_t units, int64_t t, int64_t tiles) {
+        const int64_t group = worker / kAttendWaves * kAttendWaves, mine = first(worker, units);
+        return t - (mine - first(group, units)) > 0 && t + (first(group + kAttendWaves, units) - mine) < tiles;
+    }
 };
+
+// The partial results of a pair of the workers first .. last.  A worker leaves at most two: of the pair that an earlier worker began (slot 2 w) and of the one that
+// it begins and a later one ends (slot 2 w + 1).  With teams a workgroup in the middle of the pair leaves one, its first worker's.
+struct PairParts {
+    int first, n, alone, teams;                    // `alone` of the first worker's workgroup, or all; behind them those of the teams
+    constexpr int slot(int p) const {
+        int worker = first + p;
+        if (p >= alone) {
+            const int behind = p - alone, team = behind < teams ? behind : teams;
+            worker = (first / kAttendWaves + 1 + team) * kAttendWaves + (behind - team);
+        }
+        return 2 * worker + (p == 0);
+    }
+};
+constexpr PairParts pair_parts(int first, int last, bool teams) {
+    const int n = last - first + 1, between = last / kAttendWaves - first / kAttendWaves - 1;        // workgroups
+    if (!teams || between <= 0) return {first, n, n, 0};
+    return {first, n - (kAttendWaves - 1) * between, kAttendWaves - first % kAttendWaves, between};
+}
 
 struct AttendPlan {
     int tile;              // cache rows of a tile
@@ -92,8 +116,6 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
         return here;
     };
     p.pair_workers = take(p.joined || with_weight ? static_cast<size_t>(p.pairs) * 2 : 0);
-    // a worker leaves at most two partial results: of the pair that an earlier worker began (slot 2 w) and of the one that it begins and a
-    // later one ends (slot 2 w + 1)
     const size_t slots = p.joined ? static_cast<size_t>(2 * p.workers) * p.rows : 0;
     p.part_ml = take(slots * 2);
     p.part_o = take(slots * dh);

@@ -78,11 +78,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         at.rb = hr - at.kvh * a.row_blocks;
         at.t = __builtin_amdgcn_readfirstlane(place.at) - hr * units;
         left = __builtin_amdgcn_readfirstlane(place.left);
-        if (a.teams) {
-            const int64_t mine = D::first(worker, place.all), group = static_cast<int64_t>(blockIdx.x) * kAttendWaves;
-            const int64_t begins = at.t - (mine - D::first(group, place.all)), ends = at.t + (D::first(group + kAttendWaves, place.all) - mine);
-            team = __builtin_amdgcn_readfirstlane(begins > 0 && ends < at.tiles);
-        }
+        if (a.teams) team = __builtin_amdgcn_readfirstlane(D::in_the_middle(worker, place.all, at.t, at.tiles));
     }
     int n_ahead = WHOLE ? 0 : lens[min(at.b + 1, a.B - 1)];
     auto advance = [&](Cursor x) {

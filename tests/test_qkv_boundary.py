@@ -248,6 +248,12 @@ extern "C" int64_t workers(int64_t units) { return D::workers(units); }
 extern "C" int64_t first(int64_t w, int64_t units) { return D::first(w, units); }
 extern "C" int pair_cost() { return kAttendPairCost; }
 extern "C" int most_whole() { return kAttend4Whole; }
+extern "C" int middle(int64_t w, int64_t units, int64_t t, int64_t tiles) { return D::in_the_middle(w, units, t, tiles); }
+extern "C" int parts(int first, int last, int* slots) {
+    const PairParts p = pair_parts(first, last, true);
+    for (int i = 0; i < p.n; ++i) slots[i] = p.slot(i);
+    return p.n;
+}
 """
 
 
@@ -305,6 +311,66 @@ def test_partial_results_have_slots_of_their_own(seed):
             assert stride >= -(-(cap + 1) // tile) * tile and stride % 4 == 0 and logits - lse2 >= Bn * Hq * 4 and total - logits == -(-Bn * Hq * stride * 4 // 256) * 256
         else:
             assert logits == total
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_the_join_finds_what_workgroups_in_the_middle_of_a_pair_leave(seed):
+    """The kernel's loop over tiles, with a set of tiles for a result: all workers of a workgroup agree whether it is in the middle, every part is written once,
+    and the parts that the join reads are the pair's tiles, each once."""
+    lib = host_library(PLAN)
+    q = ctypes.c_int64
+    lib.first.restype, lib.first.argtypes, lib.middle.argtypes = q, [q, q], [q, q, q, q]
+    cost, rng, waves, most = lib.pair_cost(), random.Random(seed), 4, 2048
+    for kind in range(6):
+        longest, n = [(60000, 3), (9000, 1), (300, 40), (40, 200), (3, 2000), (5000, 16)][kind]
+        tiles = [rng.choice([1, rng.randint(1, longest), rng.randint(1, longest), longest]) for _ in range(n)]
+        begin = [0]
+        for t in tiles:
+            begin.append(begin[-1] + t + cost)
+        units, written, workers, pair = begin[-1], {}, [[None, None] for _ in tiles], 0
+        for group in range(0, most, waves):
+            teams, left_over = set(), []
+            for w in range(group, group + waves):
+                at, end = lib.first(w, units), lib.first(w + 1, units)
+                if at >= end:
+                    teams.add(False)
+                    continue
+                while begin[pair + 1] <= at:
+                    pair += 1
+                i, t = pair, at - begin[pair]
+                team = bool(lib.middle(w, units, t, tiles[i]))
+                teams.add(team)
+                if t >= tiles[i]:
+                    at, i, t = begin[i + 1], i + 1, 0
+                while at < end:                            # a pair, or the worker's part of it
+                    stop = min(end - begin[i], tiles[i])
+                    have = range(t, stop)
+                    if team:
+                        left_over.append((i, have))
+                    else:
+                        if t == 0:
+                            workers[i][0] = w
+                        if stop == tiles[i]:
+                            workers[i][1] = w
+                        if len(have) < tiles[i]:
+                            assert 2 * w + (t == 0) not in written
+                            written[2 * w + (t == 0)] = (i, [have])
+                    at, i, t = begin[i + 1], i + 1, 0
+            assert len(teams) == 1
+            if teams == {True}:
+                assert len({i for i, _ in left_over}) == 1 and len(left_over) == waves and 2 * group not in written
+                written[2 * group] = (left_over[0][0], [have for _, have in left_over])
+        slots = (ctypes.c_int * (2 * most))()
+        for i, (a, b) in enumerate(workers):
+            if a == b:
+                continue
+            found = []
+            for p in range(lib.parts(a, b, slots)):
+                of, ranges = written.pop(slots[p])
+                assert of == i
+                found += [x for r in ranges for x in r]
+            assert sorted(found) == list(range(tiles[i]))
+        assert not written
 
 
 def test_the_oracles_rows_by_hand():
