@@ -64,8 +64,9 @@ METOK_API int metok_rotate_qk_paged(const void* q, const void* k, const void* v,
  *
  * 32 neighbouring elements of a row (32 g .. 32 g + 31) share a scale s = 2^e, the smallest power of two with max |x| <= 7 s, -100 <= e <= 100; an element
  * stands for sign * c * s with c the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the codes 0 .. 7, the sign being bit 3) to |x| / s, ties to the even code.
- * No element is further from its value than s, half of the widest step, as long as max |x| <= 7 * 2^100; larger elements become 6 * 2^100.  Rows that came out of
- * such a cache go back into one as the same values.
+ * No element is further from its value than s, half of the widest step, as long as max |x| <= 7 * 2^100; larger elements become 6 * 2^100.  Elements are
+ * numbers: an infinity becomes 6 * 2^100 (and its group's scale 2^100), and what a NaN becomes is one of the 16 codes.  Rows that came out of such a cache go back
+ * into one as the same values.
  *
  * Rows lie in blocks of 16, of 17 * dh / 2 bytes each: K and V are [B, Hkv, S_cap / 16, 17 * dh / 2] bytes each, pools [n_pages, Hkv, page_size / 16, 17 * dh / 2]:
  * S_cap and page_size are multiples of 16, whatever lengths the videos have.  A block is laid out as the lanes of the attention load it.  With w =

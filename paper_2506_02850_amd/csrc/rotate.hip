@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(const RotateArgs
 #pragma unroll
                     for (int e = 0; e < R; ++e) sum = fmaf(u[e], u[e], sum);
                     const float mean = fmaf(lanes_sum<LANES>(sum), 1.f / DH, a.eps);
-                    f = mean >= 0x1p-126f ? __builtin_amdgcn_rsqf(mean) : 0.f;
+                    f = mean < 0x1p-126f ? 0.f : __builtin_amdgcn_rsqf(mean);
                 }
 #pragma unroll
                 for (int e = 0; e < R; ++e) u[e] = fmaf(u[e], own[e], w[e] * its[e]) * f;

@@ -183,3 +183,22 @@ def test_many_videos_of_a_token_each(B):
             if start[b] < per_seq * page and 0 <= table[b, start[b] // page] < len(want):
                 want[table[b, start[b] // page], :, start[b] % page] = rows[b]
         assert same(pool[which].cpu(), want)
+
+
+def test_what_is_no_number_stays_in_its_head(B):
+    """A NaN among a normed head's elements makes the whole head NaN, and nothing else; in 4 bits an infinity is the largest value of the largest scale."""
+    x = torch.randn((2, 3, 6, 64), generator=torch.Generator().manual_seed(9)).to(torch.bfloat16).cuda()
+    x[1, 2, 1, 40] = float("nan")
+    pos = torch.ones((1, 2, 3), dtype=torch.int32, device="cuda")
+    weight = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    k, v = (torch.zeros((2, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q = B.metok_rotate_qk(x[:, :, :4], x[:, :, 4:5], x[:, :, 5:], pos, torch.rand(16, device="cuda"), k, v, q_weight=weight, k_weight=weight)["q"]
+    want = torch.zeros_like(q, dtype=torch.bool)
+    want[1, 1, 2] = True
+    assert torch.equal(q.isnan(), want) and not k.isnan().any() and not v.isnan().any()
+    k[0, 0, 0, 5], k[1, 0, 3, 60] = float("inf"), float("-inf")
+    k4, v4 = B.metok_kv4_cache(2, 1, 16, 64, "cuda")
+    B.metok_kv4_pack(k, v, k4, v4)
+    back = B.metok_kv4_unpack(k4, v4, torch.full((2,), 16, dtype=torch.int32, device="cuda"), 16)["k"]
+    assert back[0, 0, 0, 5] == 6 * 2.0 ** 100 and back[1, 0, 3, 60] == -6 * 2.0 ** 100 and back.isfinite().all()
+    assert (back[0, 0, 0, :32].count_nonzero(), back[1, 0, 3, 32:].count_nonzero()) == (1, 1) and back[0, 0, 0, 32:].any()
