@@ -68,7 +68,7 @@ __device__ __forceinline__ Place find_place(const DecodeArgs& a, int worker) {
         const bool in = b0 + lane < a.B;
         n = in ? rows_before(a, b0 + lane) : 0;
         tiles = max(static_cast<int>(static_cast<uint32_t>(n + fresh + TILE - 1) / TILE), 1);
-        const int units = in ? tiles + kAttendPairCost : 0;
+        const int units = in ? tiles + DEAL::kPairCost : 0;
         const int incl = wave_inclusive_scan(units);
         before = incl - units;
         return __builtin_amdgcn_readlane(incl, 63);
@@ -82,7 +82,7 @@ __device__ __forceinline__ Place find_place(const DecodeArgs& a, int worker) {
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         int sum = total;
         if (a.B > 64) sum = look(b0);
-        const unsigned long long hit = __ballot(b0 + lane < a.B && static_cast<int64_t>(base + before + tiles + kAttendPairCost) * heads > first);
+        const unsigned long long hit = __ballot(b0 + lane < a.B && static_cast<int64_t>(base + before + tiles + DEAL::kPairCost) * heads > first);
         if (hit) {
             const int l = __builtin_amdgcn_readfirstlane(__ffsll(static_cast<long long>(hit)) - 1);
             p.b = b0 + l;

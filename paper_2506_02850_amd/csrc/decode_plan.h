@@ -31,15 +31,15 @@ constexpr int kAttendWholeWaves = 8, kAttendWhole = 32;
 // Worker w of n has units [w T / n, (w + 1) T / n), or kAttendMinTiles of them where there are few (2307 rows of 28 heads on 4: 9.2 us with one, 9.3
 // with two, 11 with four; 2 x 5033 of 14 on 2 in fp32: 12.3, 10.7, 11.1: with one there are more parts to join).
 constexpr int kAttendMinTiles = 2, kAttendPairCost = 1;
-template <int GROUPS> struct Deal {
-    static constexpr int kWorkers = GROUPS * kAttendWaves;
+template <int GROUPS, int MIN_TILES = kAttendMinTiles, int PAIR_COST = kAttendPairCost> struct Deal {
+    static constexpr int kWorkers = GROUPS * kAttendWaves, kPairCost = PAIR_COST;
     static_assert((kWorkers & (kWorkers - 1)) == 0, "a worker's first unit is a shift away");
     static constexpr int64_t workers(int64_t units) {
-        const int64_t few = (units + kAttendMinTiles - 1) / kAttendMinTiles;
+        const int64_t few = (units + MIN_TILES - 1) / MIN_TILES;
         return few < kWorkers ? few : kWorkers;
     }
     static constexpr int64_t first(int64_t worker, int64_t units) {
-        const int64_t at = units < static_cast<int64_t>(kAttendMinTiles) * kWorkers ? worker * kAttendMinTiles : worker * units / kWorkers;
+        const int64_t at = units < static_cast<int64_t>(MIN_TILES) * kWorkers ? worker * MIN_TILES : worker * units / kWorkers;
         return at < units ? at : units;
     }
     // Whether a worker's whole workgroup, of kAttendWaves workers that follow each other, is in the middle of the pair in which the worker begins at tile t.
@@ -86,8 +86,9 @@ struct AttendPlan {
 };
 
 // What the split goes by beside the shapes: cache rows of a tile, workgroups of a large call, blocks of 16 query heads that a wave takes at a time where a
-// kv head has more than one, up to how many tiles a pair is left to one workgroup, and whether the workers of a workgroup may join what they leave of a pair.
-struct AttendSplit { int tile, groups, blocks, whole; bool teams; };
+// kv head has more than one, up to how many tiles a pair is left to one workgroup, units a worker has at least and a pair's end counts, and whether the workers of
+// a workgroup may join what they leave of a pair.
+struct AttendSplit { int tile, groups, blocks, whole, min_tiles, pair_cost; bool teams; };
 
 // `capacity` rows at most, one more with a new row.
 constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh, const AttendSplit& split, bool with_weight) {
@@ -103,7 +104,7 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
     p.whole = !p.wide && !with_weight && most <= split.whole;
     p.joined = most > 1 && !p.whole;
     const int groups = split.groups;
-    const int64_t few = ((most + kAttendPairCost) * p.pairs + kAttendMinTiles - 1) / kAttendMinTiles;      // workers, with a workgroup each
+    const int64_t few = ((most + split.pair_cost) * p.pairs + split.min_tiles - 1) / split.min_tiles;      // workers, with a workgroup each
     p.grid = few < groups ? few : groups;
     p.teams = split.teams && few > groups;
     p.workers = static_cast<int64_t>(groups) * kAttendWaves;
@@ -125,7 +126,7 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
     return p;
 }
 constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int dh, int esize, bool with_weight) {
-    return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole, false}, with_weight);
+    return plan_split(B, Hq, Hkv, capacity, dh, {attend_tile(esize, dh), attend_groups(esize, dh), attend_blocks(dh, Hq / Hkv), kAttendWhole, kAttendMinTiles, kAttendPairCost, false}, with_weight);
 }
 
 // The same over a cache in 4 bits (kv4_attention.hip).  A row has a quarter of the bytes, so it takes two waves to a SIMD to keep enough of them on their way, and
@@ -135,8 +136,13 @@ constexpr int kAttend4Tile = 32, kAttend4Groups = 512;
 // A pair per workgroup up to 32 tiles, as above.  28 heads on 4 of 128: 120 rows 5.1 us (10.4 split and joined), 1000 rows 8.3 (10.6), 16 of them 9.1
 // (12.0), 64 of them 10.8 (19.6); 2000 rows 12.5 (9.9), 16 of them 14.0 (13.4), 64 of them 16.5 (24.2).
 constexpr int kAttend4Whole = 32;
+// A tile is read in a quarter of the time, and what a worker does before the first and behind the last one counts for more: tiles go to workers one by one where they are
+// few, and a pair's end is two of them (8 x 700 to 3000 rows of 256 elements 8.6 us with two tiles at least and an end of one, 7.7 with one and one, 7.4 with one
+// and two, 7.2 with one and three; 32 videos of 0 to 8191 rows 15.8, 15.7, 14.0, 14.1; 2307 rows 5.5, 5.5, 5.3, 5.6).
+constexpr int kAttend4MinTiles = 1, kAttend4PairCost = 2;
+typedef Deal<kAttend4Groups, kAttend4MinTiles, kAttend4PairCost> Deal4;
 constexpr AttendPlan plan_attend4(int B, int Hq, int Hkv, int64_t capacity, int dh, bool with_weight) {
-    return plan_split(B, Hq, Hkv, capacity, dh, {kAttend4Tile, kAttend4Groups, 1, kAttend4Whole, true}, with_weight);
+    return plan_split(B, Hq, Hkv, capacity, dh, {kAttend4Tile, kAttend4Groups, 1, kAttend4Whole, kAttend4MinTiles, kAttend4PairCost, true}, with_weight);
 }
 
 }  // namespace metok

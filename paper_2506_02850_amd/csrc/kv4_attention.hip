@@ -66,13 +66,13 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         at.t = wave * at.tiles / kAttendWholeWaves;
         left = (wave + 1) * at.tiles / kAttendWholeWaves - at.t;
     } else {
-        typedef Deal<kAttend4Groups> D;
+        typedef Deal4 D;
         const Place place = find_place<TILE, D>(a, worker);
         if (place.left <= 0) return;
         at.b = __builtin_amdgcn_readfirstlane(place.b);
         at.tiles = __builtin_amdgcn_readfirstlane(place.tiles);
         at.n = __builtin_amdgcn_readfirstlane(place.n);
-        const int units = at.tiles + kAttendPairCost;
+        const int units = at.tiles + kAttend4PairCost;
         const int hr = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(place.at) / static_cast<uint32_t>(units)));
         at.kvh = a.row_blocks == 1 ? hr : __builtin_amdgcn_readfirstlane(hr / a.row_blocks);
         at.rb = hr - at.kvh * a.row_blocks;
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     };
 
     if (!WHOLE && at.t >= at.tiles) {                      // behind a pair: on to the next one, if there is one
-        left -= at.tiles + kAttendPairCost - at.t;
+        left -= at.tiles + kAttend4PairCost - at.t;
         if (left <= 0) return;
         at.t = at.tiles - 1;
         at = advance(at);
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         load_v(at, rows);
         for (;;) {
             const bool ends = !WHOLE && at.t == at.tiles - 1;
-            left -= ends ? 1 + kAttendPairCost : 1;
+            left -= ends ? 1 + kAttend4PairCost : 1;
             const bool last = left <= 0;
             // Behind the last tile the first one of all is loaded, for nobody: with loads that may not be there the waits for those before them would wait for
             // everything (8 x 36992 rows, 28 heads on 4 of 128: 47 us).

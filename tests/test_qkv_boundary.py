@@ -243,10 +243,10 @@ extern "C" void attend_plan(int B, int Hq, int Hkv, int64_t cap, int dh, int w, 
     for (int64_t v : {int64_t(p.tile), int64_t(p.row_blocks), int64_t(p.block_rows), int64_t(p.rows), p.pairs, p.grid, p.workers, int64_t(p.joined), p.logit_stride, int64_t(p.pair_workers),
                       int64_t(p.part_ml), int64_t(p.part_o), int64_t(p.lse2), int64_t(p.logits), int64_t(p.bytes), int64_t(p.whole)}) *o++ = v;
 }
-typedef Deal<kAttend4Groups> D;
+typedef Deal4 D;
 extern "C" int64_t workers(int64_t units) { return D::workers(units); }
 extern "C" int64_t first(int64_t w, int64_t units) { return D::first(w, units); }
-extern "C" int pair_cost() { return kAttendPairCost; }
+extern "C" int pair_cost() { return kAttend4PairCost; }
 extern "C" int most_whole() { return kAttend4Whole; }
 extern "C" int middle(int64_t w, int64_t units, int64_t t, int64_t tiles) { return D::in_the_middle(w, units, t, tiles); }
 extern "C" int parts(int first, int last, int* slots) {
