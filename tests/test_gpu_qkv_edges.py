@@ -202,3 +202,13 @@ def test_what_is_no_number_stays_in_its_head(B):
     back = B.metok_kv4_unpack(k4, v4, torch.full((2,), 16, dtype=torch.int32, device="cuda"), 16)["k"]
     assert back[0, 0, 0, 5] == 6 * 2.0 ** 100 and back[1, 0, 3, 60] == -6 * 2.0 ** 100 and back.isfinite().all()
     assert (back[0, 0, 0, :32].count_nonzero(), back[1, 0, 3, 32:].count_nonzero()) == (1, 1) and back[0, 0, 0, 32:].any()
+
+
+def test_long_videos_of_many_heads_and_of_pages_that_are_none(B):
+    """Several blocks of query heads to a kv head, each split over many workgroups; and whole workgroups that find no row."""
+    go(B, K.make("bf16", [9000, 70], 33, 1, 64, 9008, seed=1))
+    go(B, K.make("f32", [5000], 40, 2, 32, 5008, 16, append=False, weights=True, seed=2))
+    broken = [(0, p, -1 - p) for p in range(10, 110)] + [(1, p, -1) for p in range(128)]
+    go(B, K.make("bf16", [8191, 8000], 8, 2, 128, 8192, 64, broken=broken, seed=3))
+    res = go(B, K.make("bf16", [8192, 8000], 8, 2, 128, 8192, 64, append=False, broken=broken, seed=4))
+    assert (res["out"][1] == 0).all() and torch.isneginf(res["lse"][1]).all()
