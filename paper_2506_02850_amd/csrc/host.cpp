@@ -543,12 +543,13 @@ PyObject* decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
 inline const int32_t* per_video(PyObject* o, int64_t B, const at::Tensor& like) {
     return given(o) ? static_cast<const int32_t*>(address(fitting(o, at::kInt, {B}, like))) : nullptr;
 }
-// The page table of a paged call.
+// The page table of a paged call.  One without columns has no address, and the call that it belongs to is a paged one all the same, which the library refuses.
 struct Table {
+    const bool paged;
     const int32_t* p = nullptr;
     int per_seq = 0;
-    Table(PyObject* o, int64_t B, const at::Tensor& like) {
-        if (!given(o)) return;
+    Table(PyObject* o, int64_t B, const at::Tensor& like) : paged(given(o)) {
+        if (!paged) return;
         const at::Tensor& t = beside(tensor(o), like);
         need(t.scalar_type() == at::kInt && t.dim() == 2 && t.size(0) == B && t.size(1) <= INT32_MAX);
         p = static_cast<const int32_t*>(address(t));
@@ -588,7 +589,7 @@ PyObject* rotate_qk(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         need(k_to.dim() == 4 && k_to.scalar_type() == type && k_to.size(1) == k.heads && k_to.size(3) == dh && k_to.size(2) <= INT32_MAX);
         const at::Tensor& v_to = fitting(a[6], type, k_to.sizes(), like);
         const Table table(a[7], B, like);
-        need(table.p || k_to.size(0) == B);
+        need(table.paged || k_to.size(0) == B);
         const at::Tensor &pos = beside(tensor(a[3]), like), &freq = beside(tensor(a[4]), like);
         need(pos.scalar_type() == at::kInt && (pos.dim() == 3 || pos.dim() == 2) && pos.size(-2) == B && pos.size(-1) == n && freq.scalar_type() == at::kFloat && freq.dim() == 1);
         const int64_t axes = pos.dim() == 3 ? pos.size(0) : 1, half = freq.size(0);
@@ -613,7 +614,7 @@ PyObject* rotate_qk(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
                          static_cast<const int32_t*>(address(pos)), static_cast<int>(axes), static_cast<const float*>(address(freq)), axis, static_cast<int>(2 * half), pairs,
                          address(to), address(k_to), address(v_to), tail..., start, stream);
         };
-        return answer(table.p ? launch(call(&metok_rotate_qk_paged, k_to.size(0), static_cast<int>(k_to.size(2)), table.p, table.per_seq))
+        return answer(table.paged ? launch(call(&metok_rotate_qk_paged, k_to.size(0), static_cast<int>(k_to.size(2)), table.p, table.per_seq))
                               : launch(call(&metok_rotate_qk, k_to.size(2))), r);
     });
 }
@@ -644,7 +645,7 @@ PyObject* kv4_pack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         const int64_t B = k.size(0);
         need(to.Hkv == k.size(1) && to.dh == k.size(3));
         const Table table(a[4], B, k);
-        need(table.p || to.slabs == B);
+        need(table.paged || to.slabs == B);
         const int32_t *start = per_video(a[5], B, k), *count = per_video(a[6], B, k), *idx = nullptr;
         int64_t n = k.size(2);
         if (given(a[7])) {
@@ -658,7 +659,7 @@ PyObject* kv4_pack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         auto call = [&](auto f, auto... tail) {
             return bound(f, address(k), address(v), static_cast<int>(B), to.Hkv, k.size(2), to.dh, dt, idx, n, count, address(to.k), address(to.v), tail..., start, stream);
         };
-        return answer(table.p ? launch(call(&metok_kv4_pack_paged, to.slabs, static_cast<int>(to.rows), table.p, table.per_seq)) : launch(call(&metok_kv4_pack, to.rows)), done);
+        return answer(table.paged ? launch(call(&metok_kv4_pack_paged, to.slabs, static_cast<int>(to.rows), table.p, table.per_seq)) : launch(call(&metok_kv4_pack, to.rows)), done);
     });
 }
 
@@ -670,7 +671,7 @@ PyObject* kv4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
         need(lens.scalar_type() == at::kInt && lens.dim() == 1 && lens.size(0) <= INT32_MAX);
         const int64_t B = lens.size(0), n = integer(a[4]);
         const Table table(a[2], B, from.k);
-        need(table.p || from.slabs == B);
+        need(table.paged || from.slabs == B);
         const Outputs out(a[7], from.k);
         PyObject *ko = out.find("k"), *vo = out.find("v");
         need(ko && vo);
@@ -686,7 +687,7 @@ PyObject* kv4_unpack(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
             return bound(f, address(from.k), address(from.v), static_cast<int>(B), from.Hkv, middle..., static_cast<const int32_t*>(address(lens)), first, idx, n,
                          address(k), address(v), k.size(2), dt, stream);
         };
-        return answer(table.p ? launch(call(&metok_kv4_unpack_paged, from.slabs, static_cast<int>(from.rows), from.dh, table.p, table.per_seq))
+        return answer(table.paged ? launch(call(&metok_kv4_unpack_paged, from.slabs, static_cast<int>(from.rows), from.dh, table.p, table.per_seq))
                               : launch(call(&metok_kv4_unpack, from.rows, from.dh)), r);
     });
 }

@@ -145,3 +145,31 @@ def test_attention_calls(monkeypatch, form):
             run()
         return
     check_same(*both(monkeypatch, run, [True, form != "numpy_scale"]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("call", ["rotate", "pack", "unpack", "attention"])
+def test_tables_without_pages_are_refused(monkeypatch, call, native):
+    """A table of no columns is a table: the call is refused, also where the pool has as many pages as there are videos, and nothing is written."""
+    if not native:
+        monkeypatch.setattr(B, "_host", type("Declines", (), {"__getattr__": lambda self, name: lambda *a: None})())
+    g = torch.Generator(device="cuda").manual_seed(4)
+    lens, pos, freq = ints([3, 2]), ints([[[0, 1], [2, 3]]]), torch.rand(32, generator=g, device="cuda")
+    for table in (torch.zeros((2, 0), dtype=torch.int32, device="cuda"), ints([[1, 0], [0, 1]])[:, :0]):
+        if call == "rotate":
+            qkv, pool, out = cuda(2, 2, 6, 64, g=g), cuda(2, 2, 2, 16, 64, g=g), {"q": cuda(2, 2, 2, 64, g=g)}
+            args, kw = (B.metok_rotate_qk_paged, qkv[:, :, :2], qkv[:, :, 2:4], qkv[:, :, 4:], pos, freq, pool[0], pool[1], table), dict(out=out)
+        else:
+            pool, out = torch.randint(100, 140, (2, 2, 2, 1, 544), generator=g, device="cuda", dtype=torch.uint8), {x: cuda(2, 2, 2, 64, g=g) for x in "kv"}
+            rows = cuda(2, 2, 2, 2, 64, g=g)
+            args, kw = {"pack": ((B.metok_kv4_pack_paged, rows[0], rows[1], pool[0], pool[1], table), {}),
+                        "unpack": ((B.metok_kv4_unpack_paged, pool[0], pool[1], table, lens, 2), dict(out=out)),
+                        "attention": ((B.metok_kv4_attention_paged, rows[0, :, :, 0], pool[0], pool[1], table, lens), dict(k_new=rows[1, :, :, 0].contiguous(),
+                                                                                                                     v_new=rows[1, :, :, 1].contiguous()))}[call]
+            args = tuple(x.contiguous() if isinstance(x, torch.Tensor) and x is not table else x for x in args)
+        before = [t.clone() for t in (pool, *out.values())]
+        with pytest.raises(B.MetokError, match="page_table|capacity|pages_per_seq"):
+            args[0](*args[1:], **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(before, (pool, *out.values())))
