@@ -177,8 +177,9 @@ __global__ __launch_bounds__(kRotateThreads) void rotate_kernel(const RotateArgs
                     const float mean = fmaf(lanes_sum<LANES>(sum), 1.f / DH, a.eps);
                     f = mean < 0x1p-126f ? 0.f : __builtin_amdgcn_rsqf(mean);
                 }
+                // behind the rotated elements no product: 0 times an infinity is none, and -0, unlike 0, changes no number that it is added to
 #pragma unroll
-                for (int e = 0; e < R; ++e) u[e] = fmaf(u[e], own[e], w[e] * its[e]) * f;
+                for (int e = 0; e < R; ++e) u[e] = fmaf(u[e], own[e], turned ? w[e] * its[e] : -0.f) * f;
                 y = Run<T>::pack(u);
             }
             char* to;

@@ -177,3 +177,36 @@ def test_a_captured_step_follows_its_positions(B):
         assert same(got, want) and same(kv, c["kv"])
         pos += 1
         start += 1
+
+
+def specials(dtype, shape, rng):
+    """Infinities, NaN, zeros of both signs, the smallest and the largest numbers among ordinary ones."""
+    x = torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(TORCH[dtype])
+    odd = torch.tensor([np.inf, -np.inf, np.nan, 0.0, -0.0, 1e-40, -1e-40, 3e38, -3e38], dtype=torch.float32).to(TORCH[dtype])
+    at = torch.from_numpy(rng.random(shape) < 0.4)
+    x[at] = odd[torch.from_numpy(rng.integers(0, len(odd), int(at.sum())))]
+    return x.cuda()
+
+
+@pytest.mark.parametrize("dtype,dh", [("bf16", 32), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 32), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("pairs", [Q.HALVES, Q.ADJACENT])
+@pytest.mark.parametrize("page", [0, 16])
+def test_what_is_not_rotated_is_copied(B, dtype, dh, pairs, page):
+    """Without a norm, the elements behind the rotated ones stay what they are, whatever they are, and touch nothing else."""
+    for rot in sorted({16, dh // 32 * 16, max(16, dh - 16)}):
+        c = make(dtype, 2, 9, 5, 2, dh, rot, 3, pairs, norm=False, capacity=48, page=page, start=[3, 0], seed=rot)
+        plain = run(B, c)
+        want = [plain, c["kv"].clone()]
+        rest = specials(dtype, (2, 9, 9, dh - rot), np.random.default_rng(rot))          # 5 + 2 + 2 heads
+        c["rows"][0]._base[..., rot:] = rest
+        c["kv"].fill_(7.0)
+        got = [run(B, c), c["kv"]]
+        want[0][..., rot:] = rest[:, :, :5].transpose(1, 2)
+        for b in range(2):
+            for i in range(9):
+                j = (c["start"][b]) + i
+                slab, row = (int(c["table"][b, j // page]), j % page) if page else (b, j)
+                want[1][0, slab, :, row, rot:], want[1][1, slab, :, row, rot:] = rest[b, i, 5:7], rest[b, i, 7:]
+        for x, y in zip(got, want):
+            assert torch.equal(x.isnan(), y.isnan()) and torch.equal(x.masked_fill(x.isnan(), 0.5), y.masked_fill(y.isnan(), 0.5))
+            assert torch.equal(x.signbit() & ~x.isnan(), y.signbit() & ~y.isnan())
