@@ -123,7 +123,8 @@ METOK_API int metok_kv4_unpack_paged(const void* k_pool, const void* v_pool, int
  *   k_cache, v_cache  the 4-bit cache, S_cap a multiple of 16.
  *   k_new, v_new  rows of `dtype`, which the call puts into 4 bits: what is stored at row len[b] is also what is attended to.
  *   Results are those of the values that the cache stands for (products of `dtype` queries with them, accumulated in fp32; in fp32 with all bits of the queries
- *   and probabilities).  2^102 * dh * |q| has to be finite.
+ *   and probabilities).  Finite in fp32 have to be: 2^103 * dh * max |q_e| (a value reaches 6 * 2^100) and 1.45 s_j; and 2^8 times the sum of the magnitudes of an
+ *   element of V over a video's rows, since a probability may be relative to a maximum that is 2^8 times smaller than the last one (up to 170000 rows of 6 * 2^100).
  *   Limit: B * Hkv * ceil(Hq / Hkv / 16) * (S_cap / 16 + 4) below 2^31.
  *   workspace    metok_kv4_attention_workspace_bytes().
  */

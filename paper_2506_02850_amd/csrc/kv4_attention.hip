@@ -331,8 +331,8 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
         float top = s[0][0];
 #pragma unroll
         for (int i = 1; i < NV; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
-        // What probabilities are relative to follows the maximum only where that is more than 2^kLag times it: sums and products are fp32 numbers of any
-        // size, and with several heads some maximum grows in most tiles of a short run.
+        // What probabilities are relative to follows the maximum only where that is more than 2^kLag times it: with several heads some maximum grows in most
+        // tiles of a short run, and fp32 sums have room for probabilities of up to 2^kLag (as long as that many times the values' magnitudes add up to an fp32 number).
         constexpr float kLag = 8.f;
         if (__any((top - m) * scale > kLag)) {
             const float to = fmaxf(m, rows_max(top)), g = exp2_from(m, to == -INFINITY ? 0.f : to, scale);

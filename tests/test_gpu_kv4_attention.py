@@ -151,3 +151,54 @@ def test_a_captured_loop_is_the_eager_one(B):
             torch.cuda.synchronize()
             assert same(out["out"], want["out"]) and same(out["lse"], want["lse"]), step
         assert same(c["k"], eager["k"]) and same(c["v"], eager["v"]) and same(c["weight"], eager["weight"])
+
+
+@pytest.mark.parametrize("dtype,dh", KINDS)
+@pytest.mark.parametrize("rows,page", [(700, 0), (3000, 32)])
+def test_the_largest_scores_and_values(B, dtype, dh, rows, page):
+    """Queries and values at the end of the documented range: rows that agree with the query in every sign, all alike, have the whole weight, the others, which disagree,
+    none.  Equal rows have equal scores, so the result is these rows' value: off by its rounding, by that of the sums of up to two (fp32: three) products for 32 rows
+    and by some 64 roundings on the way; the scores are sums of dh (fp32: 3 dh) products of one sign."""
+    big, capacity = 6 * 2.0 ** 100, -(-rows // 32) * 32 + 32
+    g = torch.Generator().manual_seed(dh)
+    sign = torch.randint(0, 2, (2, dh), generator=g) * 2.0 - 1.0
+    q = (sign[0] * (2.0 ** 25 / dh * (1 - 2 * K.HALF[dtype]))).to(K.TORCH[dtype]).expand(1, 4, dh).contiguous().cuda()
+    assert 2.0 ** 102 * dh * float(q.abs().max()) < 2.0 ** 127 and float(q.abs().max()) >= 2.0 ** 25 / dh * (1 - 2.0 ** -6)
+    with_it = torch.randint(0, 2, (rows,), generator=g).bool()
+    k = torch.where(with_it[:, None], big * sign[0], -big * sign[0]).to(K.TORCH[dtype])
+    v = torch.where(with_it[:, None], big * sign[1], -big).to(K.TORCH[dtype])
+    k, v = (x.expand(1, 2, rows, dh).contiguous().cuda() for x in (k, v))
+    lens = torch.tensor([rows], dtype=torch.int32, device="cuda")
+    if page:
+        table = torch.randperm(capacity // page, generator=g).int().view(1, -1).cuda()
+        four = [t.fill_(130) for t in B.metok_kv4_cache(capacity // page, 2, page, dh, "cuda")]
+        B.metok_kv4_pack_paged(k, v, *four, table)
+        res = B.metok_kv4_attention_paged(q, *four, table, lens)
+    else:
+        four = [t.fill_(130) for t in B.metok_kv4_cache(1, 2, capacity, dh, "cuda")]
+        B.metok_kv4_pack(k, v, *four)
+        res = B.metok_kv4_attention(q, *four, lens)
+    want = (big * sign[1]).double()
+    parts = (1, 2) if dtype == "bf16" else (3, 3)
+    tol = K.HALF[dtype] + (parts[1] * rows / 32 + 64) * K.U
+    assert (res["out"].double().cpu() - want).abs().max() <= tol * big
+    score = float(q.double().abs()[0, 0].sum()) * big * dh ** -0.5
+    assert (res["lse"].double().cpu() - score - float(with_it.sum().double().log())).abs().max() <= (parts[0] * dh + 8) * K.U * score
+
+
+def test_sums_of_the_largest_values_over_a_long_cache(B):
+    """160000 rows of the largest value, whose scores grow by almost 2^8 within the tiles' runs: the sums stay finite, and the result is the value,
+    off by its rounding and by at most one rounding for each of the two products of 32 rows and 64 more; the sum of the probabilities likewise."""
+    rows, dh, big = 160000, 32, 6 * 2.0 ** 100
+    at = torch.arange(rows, device="cuda")
+    for run in (32, 96, 80000):
+        high = (at // run) % 2 == 1
+        k = torch.where(high[:, None], 1.0, 0.0).expand(rows, dh).to(torch.bfloat16).expand(1, 1, rows, dh).contiguous()
+        v = torch.full((1, 1, rows, dh), big, dtype=torch.bfloat16, device="cuda")
+        q = torch.full((1, 2, dh), 1.0, dtype=torch.bfloat16, device="cuda")
+        four = B.metok_kv4_cache(1, 1, rows, dh, "cuda")
+        B.metok_kv4_pack(k, v, *four)
+        res = B.metok_kv4_attention(q, *four, torch.tensor([rows], dtype=torch.int32, device="cuda"), scale=7.99 / 1.4426950408889634 / dh)
+        assert (res["out"].double() - big).abs().max() <= (2.0 ** -8 + (2 * rows / 32 + 64) * K.U) * big
+        want = torch.log(high.sum().double() * 2 ** 7.99 + (~high).sum().double())
+        assert (res["lse"].double() - want).abs().max() <= (2 * rows / 32 + 64) * K.U
