@@ -53,7 +53,7 @@ class Cache4:
         return t[0], t[1], None if self.table is None else torch.from_numpy(self.table.copy()).cuda()
 
 
-def make(dtype, lens, Hq, Hkv, dh, capacity, page=0, append=True, weights=False, cap=0.0, spread=2.0, seed=0, broken=()):
+def make(dtype, lens, Hq, Hkv, dh, capacity, page=0, append=True, weights=False, cap=0.0, spread=2.0, seed=0, broken=(), kind=Cache4):
     """The inputs of one attention over 4 bits, on the device, and what they are in float64.  broken: (video, page index, entry) of the table that are no
     pages of the pool."""
     rng = np.random.default_rng(seed)
@@ -61,7 +61,7 @@ def make(dtype, lens, Hq, Hkv, dh, capacity, page=0, append=True, weights=False,
     q, q64 = typed(spread * rng.standard_normal((B, Hq, dh)), dtype)
     kn, kn64 = typed(rng.standard_normal((B, Hkv, dh)), dtype)
     vn, vn64 = typed(rng.standard_normal((B, Hkv, dh)), dtype)
-    cache = Cache4(B, Hkv, capacity, dh, page, seed)
+    cache = kind(B, Hkv, capacity, dh, page, seed)
     for b, p, entry in broken:
         cache.table[b, p] = entry
     held, rows = [min(max(n, 0), capacity) for n in lens], [[], []]

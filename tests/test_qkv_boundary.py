@@ -12,6 +12,7 @@ import pytest
 import torch  # noqa: F401  (loaded first so that the library binds to the same HIP runtime)
 
 from oracle import qkv_oracle as Q
+from tests import kv4_large as large
 from tests.host_plan import host_library
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -420,3 +421,56 @@ def test_the_oracles_rotation_by_hand():
     q, k = rng.standard_normal((2, 1, 1, 32))
     dots = [float((Q.rotate(q, None, 0, [[p]], freq, [0] * 8, 0) * Q.rotate(k, None, 0, [[p + 7]], freq, [0] * 8, 0)).sum()) for p in (0, 5, 1000)]
     np.testing.assert_allclose(dots, dots[0], rtol=1e-10)
+
+
+def walk(lib, tiles):
+    """The kernel's loop for pairs of so many tiles: of every worker, its pieces (pair, tiles) and whether its workgroup is in the middle of a pair."""
+    cost, begin = lib.pair_cost(), [0]
+    for t in tiles:
+        begin.append(begin[-1] + t + cost)
+    units, pair, found = begin[-1], 0, []
+    for w in range(lib.workers(units)):
+        at, end, pieces = lib.first(w, units), lib.first(w + 1, units), []
+        while begin[pair + 1] <= at:
+            pair += 1
+        i, team = pair, bool(lib.middle(w, units, at - begin[pair], tiles[pair]))
+        while at < end:
+            have = range(at - begin[i], min(end - begin[i], tiles[i]))
+            if have:
+                pieces.append((i, have))
+            i += 1
+            at = begin[i]
+        found.append((pieces, team))
+    return units, found
+
+
+@pytest.mark.parametrize("name", sorted(large.CASES))
+def test_the_large_cases_give_a_worker_several_tiles(name):
+    """What tests/test_gpu_kv4_large.py is for: several tiles of a pair to a worker, several pairs and videos, teams of several tiles, rows that are appended before the
+    last tile of a worker.  A split that is tuned anew must not empty it."""
+    lib = host_library(PLAN)
+    q = ctypes.c_int64
+    lib.workers.restype, lib.workers.argtypes, lib.first.restype, lib.first.argtypes, lib.middle.argtypes = q, [q], q, [q, q], [q, q, q, q]
+    dtype, lens, Hq, Hkv, dh, capacity, kw = large.CASES[name]
+    o = (q * 16)()
+    lib.attend_plan(len(lens), Hq, Hkv, q(capacity), dh, int(kw.get("weights", False)), o)
+    tile, row_blocks, whole, most = o[0], o[1], o[15], o[6]
+    fresh = int(kw.get("append", True))
+    tiles = [max(1, -(-(min(n, capacity) + fresh) // tile)) for n in lens for _ in range(Hkv * row_blocks)]
+    units, workers = walk(lib, tiles)
+    assert not whole and units > 2 * most and len(workers) == most
+    assert max(len(have) for pieces, _ in workers for _, have in pieces) > 1
+    crossing = [pieces for pieces, _ in workers if len(pieces) > 1]
+    assert crossing
+    if "short" in name or "ragged" in name:
+        assert any(len({i // (Hkv * row_blocks) for i, _ in pieces}) > 1 for pieces in crossing) and len(lens) > 64
+    if name == "short_pairs":
+        assert any(len(pieces) > 2 for pieces in crossing)
+    if "long" in name or "three" in name:
+        assert any(team and len(pieces[0][1]) > 1 for pieces, team in workers)
+    if "three" in name:
+        assert row_blocks == 3
+    if fresh:                                              # the new row's tile, and tiles of the same worker behind it
+        assert any(have[-1] + 1 == tiles[i] and (i, have) != pieces[-1] for pieces, _ in workers for i, have in pieces)
+    if "streamed" in name:
+        assert len(lens) * Hkv * capacity * dh * 17 // 16 > 128 << 20
