@@ -108,8 +108,7 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
     p.grid = few < groups ? few : groups;
     p.teams = split.teams && few > groups;
     p.workers = static_cast<int64_t>(groups) * kAttendWaves;
-    const int rounded = p.tile > 32 ? p.tile : 32;                                   // whole tiles are written
-    p.logit_stride = with_weight ? (capacity + 1 + rounded - 1) / rounded * rounded : 0;
+    p.logit_stride = with_weight ? (capacity + 1 + 31) / 32 * 32 : 0;                // whole tiles are written, of 16 or 32 rows
     size_t at = 0;
     auto take = [&at](size_t floats) {
         const size_t here = at;
@@ -133,6 +132,7 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
 // tiles of 32 rows at any width (28 heads on 4 of 128, 8 x 36992 rows: 31.3 us with 512 workgroups, 41.3 with 256; 32 videos of 0 to 8191 rows 15.6 and 19.5.  Tiles
 // of 64 rows in 256 workgroups take as long at 8 x 36992, but 2307 rows 6.2 us against 5.4, 8 x 3000 of 256 elements 11.3 against 8.4).
 constexpr int kAttend4Tile = 32, kAttend4Groups = 512;
+static_assert(32 % kAttend4Tile == 0, "32 logits hold whole tiles");
 // A pair per workgroup up to 32 tiles, as above.  28 heads on 4 of 128: 120 rows 5.1 us (10.4 split and joined), 1000 rows 8.3 (10.6), 16 of them 9.1
 // (12.0), 64 of them 10.8 (19.6); 2000 rows 12.5 (9.9), 16 of them 14.0 (13.4), 64 of them 16.5 (24.2).
 constexpr int kAttend4Whole = 32;

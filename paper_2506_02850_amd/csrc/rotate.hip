@@ -9,7 +9,7 @@
 
 namespace metok {
 
-constexpr int kRotateThreads = 256, kRotateWaves = kRotateThreads / 64;
+constexpr int kRotateThreads = 256;
 constexpr int kRotUnit = 16, kMaxPairs = 128;              // rot is a multiple of; pairs of a head at most
 constexpr int kAtOnce = 4;                                 // heads whose loads are on their way together
 // Heads that a workgroup takes where there are kRotateSpread workgroups of one head or more: enough for the cosines and sines to be a small part of its work, few enough
