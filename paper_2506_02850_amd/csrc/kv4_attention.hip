@@ -529,18 +529,20 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
 }
 
 // Caches of more than this many bytes are read with the streaming hint: they pass through the 256 MB before memory without staying there (8 x 36992 rows of 4 heads of
-// 128, 161 MB: 31.3 us with, 33.3 without; 16 of them 59.4 and 62.2; 4 of them, 80 MB, which stay there from one call to the next, are read without).
+// 128, 161 MB: 31.3 us with, 33.3 without; 16 of them 59.4 and 62.2; 4 of them, 80 MB, which stay there from one call to the next, are read without).  A lane's load of
+// 4 or 8 bytes, of heads of 32 and 64, has no such hint.
 constexpr int64_t kStream4Bytes = 128 << 20;
 
 template <typename T, int DH, bool PAGED>
 static int launch_form(const DecodeArgs& a, const AttendPlan& plan, hipStream_t st) {
     const int64_t bytes = static_cast<int64_t>(a.B) * a.Hkv * a.S_cap * DH * 17 / 16;
     const dim3 groups(static_cast<unsigned>(plan.whole ? plan.pairs : plan.grid)), threads(kAttendThreads);
-    const bool stream = bytes > kStream4Bytes;
+    constexpr bool HINT = DH >= 128;
+    const bool stream = HINT && bytes > kStream4Bytes;
     if (plan.whole) hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, false, false, true>), groups, dim3(64 * kAttendWholeWaves), 0, st, a);
-    else if (a.weight && stream) hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, true, true, false>), groups, threads, 0, st, a);
+    else if (a.weight && stream) hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, true, HINT, false>), groups, threads, 0, st, a);
     else if (a.weight) hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, true, false, false>), groups, threads, 0, st, a);
-    else if (stream) hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, false, true, false>), groups, threads, 0, st, a);
+    else if (stream) hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, false, HINT, false>), groups, threads, 0, st, a);
     else hipLaunchKernelGGL((kv4_attention_kernel<T, DH, PAGED, false, false, false>), groups, threads, 0, st, a);
     return check_launch("attention over 4 bits");
 }

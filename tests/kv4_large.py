@@ -32,11 +32,12 @@ def _spread(n, least, most, seed):
 # name: dtype, lens, Hq, Hkv, dh, capacity, and what differs from a dense cache, to which a row is appended, without weights and cap
 CASES = {
     "long": ("bf16", [40011, 0, 30000], 12, 4, 128, 40032, {}),
-    "long_paged_streamed_f32": ("f32", [30000, 29999, 5], 16, 8, 32, 180000, dict(page=16)),
-    "long_paged_streamed_weights": ("bf16", [30011, 1], 16, 8, 64, 131072, dict(page=64, append=False, weights=True)),
+    "long_paged_streamed_f32": ("f32", [30000, 29999, 5], 8, 4, 128, 82304, dict(page=16)),
+    "long_paged_streamed_weights": ("bf16", [40011, 1], 16, 8, 128, 65536, dict(page=64, append=False, weights=True)),
     "long_weights_cap_f32": ("f32", [40000, 300], 8, 8, 64, 40016, dict(weights=True, cap=20.0)),
     "long_streamed_256": ("bf16", [26000, 12000, 40], 8, 8, 256, 26000, dict(append=False)),
-    "long_f32": ("f32", [24000, 9000], 16, 8, 128, 24000, dict(append=False, cap=30.0)),
+    "long_paged_64": ("bf16", [30011, 1], 16, 8, 64, 30016, dict(page=32)),
+    "long_f32": ("f32", [24000, 9000], 16, 8, 32, 24000, dict(append=False, cap=30.0)),
     "three_blocks_of_heads": ("bf16", [70000, 30000, 0], 40, 1, 64, 70016, {}),
     "short_pairs": ("bf16", _spread(2500, 0, 64, 1), 17, 1, 32, 64, dict(page=16)),
     "short_pairs_weights_f32": ("f32", _spread(1500, 0, 48, 2), 4, 2, 128, 48, dict(weights=True, append=False)),

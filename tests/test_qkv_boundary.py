@@ -473,4 +473,4 @@ def test_the_large_cases_give_a_worker_several_tiles(name):
     if fresh:                                              # the new row's tile, and tiles of the same worker behind it
         assert any(have[-1] + 1 == tiles[i] and (i, have) != pieces[-1] for pieces, _ in workers for i, have in pieces)
     if "streamed" in name:
-        assert len(lens) * Hkv * capacity * dh * 17 // 16 > 128 << 20
+        assert dh >= 128 and len(lens) * Hkv * capacity * dh * 17 // 16 > 128 << 20
