@@ -27,7 +27,7 @@ enum { METOK_PAIRS_HALVES = 0, METOK_PAIRS_ADJACENT = 1 };   /* which elements o
  *   q, k, v      device, of `dtype`: the rows of B * n tokens, token t = b * n + i; head h of a token's queries is q + t * q_stride + h * dh
  *                (k and v alike, Hkv heads).  The strides are in elements, multiples of 16 bytes, and at least the heads' elements; the three may
  *                be parts of one buffer, as one product leaves them.
- *   count        device, [B] int32, or NULL (= n): video b has its first count[b] tokens, of the others nothing is read or written.
+ *   count        device, [B] int32, or NULL (= n): video b has its first count[b] tokens; of the others nothing is written, and nothing but their positions may be read.
  *   q_weight, k_weight  device, [dh] of `dtype`, or both NULL (no norm): x_e becomes x_e / sqrt(mean over the head's dh elements of x^2 + eps) *
  *                weight_e.  eps in [0, 1]; a head whose mean square and eps add up to less than 2^-126 becomes zeros.
  *   pos          device, [n_axes, B, n] int32 (1 <= n_axes <= METOK_MAX_POSITION_AXES): the tokens' positions.

@@ -106,7 +106,7 @@ constexpr AttendPlan plan_split(int B, int Hq, int Hkv, int64_t capacity, int dh
     const int groups = split.groups;
     const int64_t few = ((most + split.pair_cost) * p.pairs + split.min_tiles - 1) / split.min_tiles;      // workers, with a workgroup each
     p.grid = few < groups ? few : groups;
-    p.teams = split.teams && few > groups;
+    p.teams = split.teams && few > groups;                                           // by the capacity, as the grid
     p.workers = static_cast<int64_t>(groups) * kAttendWaves;
     p.logit_stride = with_weight ? (capacity + 1 + 31) / 32 * 32 : 0;                // whole tiles are written, of 16 or 32 rows
     size_t at = 0;
@@ -133,8 +133,9 @@ constexpr AttendPlan plan_attend(int B, int Hq, int Hkv, int64_t capacity, int d
 // of 64 rows in 256 workgroups take as long at 8 x 36992, but 2307 rows 6.2 us against 5.4, 8 x 3000 of 256 elements 11.3 against 8.4).
 constexpr int kAttend4Tile = 32, kAttend4Groups = 512;
 static_assert(32 % kAttend4Tile == 0, "32 logits hold whole tiles");
-// A pair per workgroup up to 32 tiles, as above.  28 heads on 4 of 128: 120 rows 5.1 us (10.4 split and joined), 1000 rows 8.3 (10.6), 16 of them 9.1
-// (12.0), 64 of them 10.8 (19.6); 2000 rows 12.5 (9.9), 16 of them 14.0 (13.4), 64 of them 16.5 (24.2).
+// A pair per workgroup up to 32 tiles, as above.  28 heads on 4 of 128: 120 rows 5.0 us (9.6 split and joined), 1000 rows 8.2 (9.6), 16 of them 8.9
+// (11.1), 64 of them 10.4 (18.1); 2000 rows 12.1 (9.6), 16 of them 14.1 (13.0).  The rule knows the tiles and not whether the pairs alone fill the chip: 64 videos of 2000
+// rows, 256 pairs, would take 15.6 us in one launch and take 23.1.
 constexpr int kAttend4Whole = 32;
 // A tile is read in a quarter of the time, and what a worker does before the first and behind the last one counts for more: tiles go to workers one by one where they are
 // few, and a pair's end is two of them (8 x 700 to 3000 rows of 256 elements 8.6 us with two tiles at least and an end of one, 7.7 with one and one, 7.4 with one

@@ -2,9 +2,11 @@
 // chip and joined as there.
 //
 // The codes become bf16 numbers in registers, two an instruction and exactly (two bits of mantissa, scales that are powers of two), and go into the same
-// MFMA products.  What bounds it is the stream of K and V, 17 / 32 byte an element: a quarter of the time a row of bf16 takes.  The vector unit is
-// not far behind: an element of K costs half an instruction, one of V a whole one, since the values of two rows have to be brought beside each other.
-// 8 x 36992 rows, 28 query heads on 4 of 128, 161 MB: 31.3 us, 5.1 TB/s, and 4.6 for the join; 16 of them 59.4 us, 5.4 TB/s.
+// MFMA products.  The floor is the stream of K and V, 17 / 32 byte an element, a quarter of the bytes of bf16 rows.  What bounds the largest calls is the
+// issue of vector and matrix instructions beside it: an element of K costs half an instruction, one of V a whole one, since the values of two rows have to be brought beside
+// each other.  8 x 36992 rows, 28 query heads on 4 of 128, 161 MB: 31.0 us, 5.2 TB/s, as long as from rows that the caches hold, and 4.6 for the join; 16 of them 59.4 us,
+// 5.4 TB/s.  Narrower heads and fp32 queries are further from it: a tile of 32 rows costs a wave some 0.9 us at 32 elements, 1.3 at 64, 1.8 at 128, with one tile ahead at any width
+// (40 MB: 8 x 36992 rows of 4 heads of 32 18.9 us, of 2 of 64 14.6; 80 MB: 4 x 36992 of 4 of 128 18.5, 8 x 18496 in fp32, with three parts of every factor, 21.4).
 #include "decode_attention.h"
 #include "kv4.h"
 
@@ -43,8 +45,9 @@ __global__ __launch_bounds__(64 * (WHOLE ? kAttendWholeWaves : kAttendWaves), 2)
     constexpr int QP = BF16 ? 1 : 3, PP = BF16 ? 2 : 3;    // parts of a query, of a probability
     static_assert(NT % 2 == 0 && KW == EB, "32 rows to a product; a lane has as much of K as of V");
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, c = lane >> 4;
-    // Neighbouring workers on different CUs where there are few, so that few tiles are spread over all of them; in one workgroup where there are many, so that
-    // they can join what they leave of a pair that none of them begins or ends: the parts of 131072 rows are joined in 10.0 us then, not in 15.5.
+    // Neighbouring workers on different CUs where the capacity holds few tiles, so that these are spread over all of them; in one workgroup where it holds many, so
+    // that they can join what they leave of a pair that none of them begins or ends: the parts of 131072 rows are joined in 10.0 us then, not in 15.5.  A short video in a
+    // large cache has neighbours in one workgroup, too, and is not slower (2306 rows, 28 heads on 4 of 128: 4.8 us in a cache of 2560 rows, 4.9 in one of 131072).
     const int worker = a.teams ? static_cast<int>(blockIdx.x) * kAttendWaves + wave : wave * static_cast<int>(gridDim.x) + static_cast<int>(blockIdx.x);
     bool team = false;                                     // the workgroup is in the middle of a pair
     const bool fresh = a.k_new != nullptr;

@@ -14,7 +14,7 @@ constexpr int kRotUnit = 16, kMaxPairs = 128;              // rot is a multiple 
 constexpr int kAtOnce = 4;                                 // heads whose loads are on their way together
 // Heads that a workgroup takes where there are kRotateSpread workgroups of one head or more: enough for the cosines and sines to be a small part of its work, few enough
 // for the writes to stay in order (18560 tokens, 36 heads of 128, bf16: 4 heads 66.5 us, 8 64.4, 12 64.2, 20 73; 11000 of 18 of 64, fp32: 4 20.6, 8 22.1, 12 21.6;
-// without any arithmetic 62).  A step of 64 tokens, 36 heads: 5.1 us, which is launch, positions, sine and product one behind the other.
+// the prompt without norms and products, the kernel's loads, angles and stores alone, 63.4).  A step of 64 tokens, 36 heads: 5.1 us, which is launch, positions, sine and product one behind the other.
 constexpr int rotate_heads(int esize) { return 16 / esize; }
 constexpr int kRotateSpread = 4096;
 // Rows of more bytes than this are read, or written, with the streaming hint: the prompt above 64 us with both, 68 without that on the reads; the fp32 one, whose rows the
@@ -79,8 +79,8 @@ __device__ __forceinline__ void turn_of(int pos, float freq, float& cos, float& 
 
 // A lane has a run of a head of a token, the lanes of a wave the rows of neighbouring tokens, and a workgroup so many tokens of a few heads.  Workgroups with
 // neighbouring tokens follow each other, those of the next heads come behind all of them: what is written is written in the order of its addresses, 256
-// bytes and more at a time, and it is the reads that jump (18560 tokens of 36 heads of 128 in bf16, copied alone: 56 us so, 61 to 71 with the reads in order, 66
-// with a head's halves in two stores; a plain copy 53).
+// bytes and more at a time, and it is the reads that jump (18560 tokens of 36 heads of 128 in bf16, by kernels that copy and do nothing else: 56 us so, 61 to 71 with the
+// reads in order, 66 with a head's halves in two stores, 53 without any change of the order).
 //
 // The other half of a pair is with another lane.  With c, s the pair's cosine and sine, g and g' the weights of the lane's element x and of the other one x', and
 // f = 1 / root mean square, the result is f (x (g c) +- x' (g' s)): two factors to an element, computed once for all heads of a kind.
