@@ -34,7 +34,7 @@ enum { METOK_PAIRS_HALVES = 0, METOK_PAIRS_ADJACENT = 1 };   /* which elements o
  *   inv_freq     device, [rot / 2] float, finite: pair p is rotated by the angle pos[pair_axis[p]] * inv_freq[p] radians.  The product is not rounded to
  *                fp32, so that far positions keep their angles.
  *   pair_axis    host, [rot / 2] uint8 below n_axes (copied during the call), or NULL: all 0.
- *   rot          elements of a head that are rotated: a multiple of 16 and at most dh; the rest is normed, but not rotated.
+ *   rot          elements of a head that are rotated: a multiple of 16 and at most dh; the rest is normed, but not rotated (without a norm: copied, whatever it is).
  *   pairs        METOK_PAIRS_HALVES: pair p is the elements p and p + rot / 2; METOK_PAIRS_ADJACENT: 2 p and 2 p + 1.  (x, y) becomes
  *                (x cos - y sin, y cos + x sin).
  *   q_out        device out, [B, Hq, n, dh] of `dtype`, head by head as metok_prefill_prune (q_text) and, with n = 1, the attention calls take it.
